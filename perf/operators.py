@@ -1,0 +1,431 @@
+"""Attention over a paged cache as a serving program runs it, as cases that can be timed: new tokens' keys and values are
+normalised, rotated and appended, chunks and single tokens attend to everything in the cache, or to the pages that a score on
+the pages' bounds selects.
+
+``own`` False: the operators in plain torch operations; True: the library's calls.
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+THETA, EPS = 10000.0, 1e-6
+
+
+def listed():
+    return [
+        # one decoding step of 64 sequences: their new keys and values, normalised per head and rotated
+        _case("append_64x1_32x128", "append", "bf16", B=64, H=32, H_kv=8, d_h=128, page=16, new=(1, 1), past=(1, 1023), rot=128, pairs=False, norm=True),
+        # four prompts of 2048 tokens, heads of 256 with a quarter of each rotated in neighbouring pairs
+        _case("append_4x2048_16x256", "append", "bf16", B=4, H=16, H_kv=16, d_h=256, page=64, new=(2048, 2048), past=(0, 0), rot=64, pairs=True, norm=False),
+        # a small model's prompt in fp32
+        _case("append_f32_512_12x64", "append", "f32", B=1, H=12, H_kv=12, d_h=64, page=16, new=(512, 512), past=(0, 0), rot=64, pairs=False, norm=False),
+        # the smallest call: one token of a small model
+        _case("attend_1x1_12x64_2048", "attend", "bf16", B=1, H=12, H_kv=12, d_h=64, page=16, new=(1, 1), past=(2047, 2047), causal=True),
+        # one decoding step of 64 sequences of very different lengths
+        _case("attend_64x1_32x128", "attend", "bf16", B=64, H=32, H_kv=8, d_h=128, page=16, new=(1, 1), past=(100, 8191), causal=True),
+        # a prompt of 8192 tokens
+        _case("attend_8192_32x128", "attend", "bf16", B=1, H=32, H_kv=8, d_h=128, page=64, new=(8192, 8192), past=(0, 0), causal=True),
+        # a chunk of a long prompt behind what is in the cache already, heads of 256
+        _case("attend_512_16x256_16k", "attend", "bf16", B=1, H=16, H_kv=16, d_h=256, page=64, new=(512, 512), past=(16000, 16000), causal=True),
+        # a mixed batch: short and long chunks, odd lengths everywhere
+        _case("attend_mixed_f32_12x64", "attend", "f32", B=6, H=12, H_kv=4, d_h=64, page=32, new=(1, 333), past=(17, 1999), order="slots", causal=True),
+        # decoding with long contexts: which pages each sequence's token looks at
+        _case("select_16x1_32x128_32k", "select", "bf16", B=16, H=32, H_kv=8, d_h=128, page=64, new=(1, 1), past=(20000, 32767), causal=True, budget=32),
+        # the same for every token of a chunk
+        _case("select_2048_32x128", "select", "bf16", B=1, H=32, H_kv=8, d_h=128, page=64, new=(2048, 2048), past=(6144, 6144), causal=True, budget=16),
+        # and the attention over the selected pages
+        _case("pages_16x1_32x128_32k", "pages", "bf16", B=16, H=32, H_kv=8, d_h=128, page=64, new=(1, 1), past=(20000, 32767), causal=True, budget=32),
+        _case("pages_1024_32x128", "pages", "bf16", B=1, H=32, H_kv=8, d_h=128, page=64, new=(1024, 1024), past=(7168, 7168), causal=True, budget=16),
+    ]
+
+
+def _case(name, kind, dtype, *, new, past, order="heads", **more):
+    c = dict(kind=kind, dtype=dtype, order=order, new_lo=new[0], new_hi=new[1], past_lo=past[0], past_hi=past[1], **more)
+    return dict(c, name=name) if name else c
+
+
+def _log_between(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case: any operator, types and head layouts that the library has, lengths over their whole range."""
+    while True:
+        kind = rng.choice(("append", "attend", "attend", "select", "pages"))
+        dtype = rng.choice(("bf16", "bf16", "bf16", "f32"))
+        d_h = rng.choice((64, 128, 128, 256) if dtype == "bf16" else (64, 128))
+        H_kv = rng.choice((1, 2, 4, 5, 8, 12, 16))
+        H = H_kv * rng.choice((1, 2, 3, 4, 7, 8))
+        if H * d_h > 8192:
+            continue
+        page = rng.choice((16, 32, 64, 128)) if kind in ("append", "attend") else rng.choice((32, 64, 64, 128))
+        longest = 32767 if kind in ("select", "pages") else 16384
+        if rng.random() < 0.5:                                       # single tokens of many sequences
+            B, new = _log_between(rng, 1, 128), (1, 1)
+            past = (_log_between(rng, 1, 2000), _log_between(rng, 2000, longest))
+        else:                                                        # chunks of a few
+            B, lo = _log_between(rng, 1, 8), _log_between(rng, 1, 300)
+            new, past = (lo, _log_between(rng, lo, 4096)), (rng.choice((0, 0, 1, 77)), _log_between(rng, 100, longest // 2))
+        if kind == "append":
+            past = (min(past[0], 500), min(past[1], 1000))
+        c = _case(None, kind, dtype, B=B, H=H, H_kv=H_kv, d_h=d_h, page=page, new=new, past=past, order=rng.choice(("heads", "slots")))
+        if kind == "append":
+            rot = rng.choice((0, d_h // 4, d_h // 2, d_h, d_h))
+            c.update(rot=rot, pairs=rng.random() < 0.4, norm=rng.random() < 0.5)
+        else:
+            c["causal"] = True if kind != "attend" else rng.random() < 0.8
+        if kind in ("select", "pages"):
+            c["budget"] = _log_between(rng, 4, 64)
+            if max(a + b for a, b in zip(*_lengths(c))) // page < c["budget"] + 4:     # nothing to choose from
+                continue
+        if _cost(c) <= 1.0:
+            return c
+
+
+def _cost(c):
+    """A rough price of a case, for draw(): its share of the largest listed one, in the memory of the plain form and in products."""
+    new, past = _lengths(c)
+    n, L = sum(new), max(a + b for a, b in zip(new, past))
+    esz = 2 if c["dtype"] == "bf16" else 4
+    share = c["B"] * (L + c["page"]) * c["H_kv"] * c["d_h"] * esz / 2.5e9
+    if c["kind"] == "attend":
+        share = max(share, c["B"] * max(new) * c["H"] * L / 2.2e9, c["B"] * max(new) * c["H"] * L * c["d_h"] / 2.8e11)
+    if c["kind"] == "select":
+        share = max(share, n * c["H"] * (L / c["page"]) * c["d_h"] / 9e9)
+    if c["kind"] == "pages":
+        share = max(share, n * c["H_kv"] * c["budget"] * c["page"] * c["d_h"] / 2.2e9)
+    return share
+
+
+def _spread(lo, hi, n, by):
+    """n whole numbers over lo .. hi, evenly over their logarithm and in no order."""
+    return [int(round((lo + 1) * ((hi + 1) / (lo + 1)) ** ((j * by + 0.5 * by) % 1.0))) - 1 if hi > lo else lo for j in range(n)]
+
+
+def _lengths(c):
+    """New and cached tokens of every sequence: the same for every seed."""
+    return _spread(c["new_lo"], c["new_hi"], c["B"], 0.618034), _spread(c["past_lo"], c["past_hi"], c["B"], 0.754878)
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+def _rope_table(positions, rot):
+    """[positions, rot / 2, 2] cosines and sines; the angles in 64 bits."""
+    angle = torch.arange(positions, dtype=torch.float64, device="cuda")[:, None] * THETA ** (-torch.arange(0, rot, 2, dtype=torch.float64, device="cuda") / rot)
+    return torch.stack((angle.cos(), angle.sin()), dim=-1).float()
+
+
+def _pool(x, order):
+    """Pages [pages, H_kv, page, d_h] as they lie in memory: head by head, or token by token with the heads side by side."""
+    return x if order == "heads" else x.transpose(1, 2).contiguous().transpose(1, 2)
+
+
+def prepare(case, seed):
+    c, gen = case, torch.Generator(device="cuda").manual_seed(seed)
+    dt, B, H, H_kv, d_h, page = DTYPES[c["dtype"]], c["B"], c["H"], c["H_kv"], c["d_h"], c["page"]
+    randn = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    new, past = _lengths(c)
+    N, held = sum(new), [-(-(a + b) // page) for a, b in zip(new, past)]
+    pages = sum(held) + 3                                            # the pool has room left
+    s = dict(case=c, start=ints([sum(new[:b]) for b in range(B + 1)]), past=ints(past), longest=max(new))
+    number = torch.randperm(pages, generator=gen, device="cuda").int()
+    ends = torch.tensor(held, device="cuda").cumsum(0)
+    at = torch.arange(max(held), device="cuda")
+    s["table"] = torch.where(at < torch.tensor(held, device="cuda")[:, None], number[((ends - torch.tensor(held, device="cuda"))[:, None] + at).clamp(max=pages - 1)], -1).int().contiguous()
+    # keys of one page have something in common, as neighbouring tokens have
+    s["K"] = _pool((0.8 * randn(pages, H_kv, page, d_h) + 0.6 * randn(pages, H_kv, 1, d_h)).to(dt), c["order"])
+    s["V"] = _pool(randn(pages, H_kv, page, d_h).to(dt), c["order"])
+    if c["kind"] in ("append", "select", "pages"):
+        s["bounds"] = torch.stack((s["K"].amin(2), s["K"].amax(2)), dim=2).contiguous()
+    if c["kind"] == "append":
+        qkv = randn(N, (H + 2 * H_kv) * d_h).to(dt)                  # one projection's output
+        s["new"] = tuple(qkv.split((H * d_h, H_kv * d_h, H_kv * d_h), dim=1))
+        s["norm"] = tuple((1 + 0.1 * randn(d_h)).to(dt) for _ in range(2)) if c["norm"] else (None, None)
+        s["rope"] = _rope_table(max(a + b for a, b in zip(new, past)), c["rot"]) if c["rot"] else None
+        s["out"] = torch.zeros(N, H * d_h, dtype=dt, device="cuda")
+    else:
+        s["Q"] = randn(N, H * d_h).to(dt)
+    if c["kind"] in ("attend", "pages"):
+        s["out"] = torch.zeros(N, H * d_h, dtype=dt, device="cuda")
+    if c["kind"] == "pages":                                         # lists as a selection leaves them
+        seq, pos = _rows(s, N)
+        have = pos // page + 1
+        far = torch.rand(N, H_kv, max(held), generator=gen, device="cuda")
+        far.masked_fill_(torch.arange(max(held), device="cuda") >= have[:, None, None], 2.0)
+        far.scatter_(2, (have - 1)[:, None, None].expand(N, H_kv, 1), -1.0)
+        budget = min(c["budget"], max(held))
+        s["count"] = have.clamp(max=budget).int()[:, None].expand(N, H_kv).contiguous()
+        best = far.topk(budget, dim=2, largest=False).indices
+        best = best.masked_fill(torch.arange(budget, device="cuda") >= s["count"][:, :, None], 1 << 30).sort(dim=2).values
+        s["pages"] = torch.nn.functional.pad(best.masked_fill(best == 1 << 30, -1).int(), (0, c["budget"] - budget), value=-1).contiguous()
+    if c["kind"] == "select":
+        s["lists"] = dict(pages=torch.zeros(N, H_kv, c["budget"], dtype=torch.int32, device="cuda"), counts=torch.zeros(N, H_kv, dtype=torch.int32, device="cuda"))
+    if own:                                                          # what a program makes once: handles and a workspace
+        import paper_2605_03110_amd as pa
+        s["cache"] = pa.PagedCache(s["K"], s["V"], s.get("bounds"))
+        s["chunk"] = pa.Chunk(s["table"], s["start"], s["past"], rows=N, longest=s["longest"])
+        s["status"] = torch.zeros(1, dtype=torch.int32, device="cuda")
+        s["ws"] = pa.paged_workspace(s["cache"], s["chunk"], H)
+    return s
+
+
+# ------------------------------------------------------------------------------------------------ one pass
+def run(state):
+    c = state["case"]
+    return (_calls if own else _plain)(state, c, c["kind"])
+
+
+def _calls(s, c, kind):
+    import paper_2605_03110_amd as pa
+    flags = pa.FLAG_ATTN_CAUSAL if c.get("causal") else 0
+    if kind == "append":
+        q, k, v = s["new"]
+        pa.ada_cache_append(s["cache"], s["chunk"], q, k, v, rope=s["rope"], q_norm=s["norm"][0], k_norm=s["norm"][1], eps=EPS,
+                            out=s["out"], status=s["status"], flags=pa.FLAG_ROPE_PAIRS if c["pairs"] else 0)
+        return dict(q=s["out"], K=s["K"], V=s["V"], bounds=s["bounds"])
+    if kind == "attend":
+        return pa.ada_attention_paged(s["cache"], s["chunk"], s["Q"], ws=s["ws"], out=s["out"], status=s["status"], flags=flags)["out"]
+    if kind == "select":
+        res = pa.ada_select_pages(s["cache"], s["chunk"], s["Q"], c["budget"], first=1, last=1, ws=s["ws"], out=s["lists"], status=s["status"], flags=flags)
+        return dict(pages=res["pages"], counts=res["counts"])
+    return pa.ada_attention_pages(s["cache"], s["chunk"], s["Q"], s["pages"], s["count"], ws=s["ws"], out=s["out"], status=s["status"], flags=flags)["out"]
+
+
+def _rows(s, N):
+    """Sequence and position of every row."""
+    row = torch.arange(N, device="cuda")
+    seq = torch.searchsorted(s["start"][1:].long(), row, right=True)
+    return seq, s["past"].long()[seq] + row - s["start"].long()[seq]
+
+
+def _plain(s, c, kind):
+    return {"append": _append, "attend": _attend, "select": _select, "pages": _attend_pages}[kind](s, c)
+
+
+def _normed(x, w):
+    return x if w is None else x * torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS) * w.float()
+
+
+def _rotated(x, table, pairs):
+    """x [N, heads, d_h], table [N, rot / 2, 2]"""
+    if table is None:
+        return x
+    half = table.shape[1]
+    cos, sin = table[:, None, :, 0], table[:, None, :, 1]
+    head, rest = x[..., :2 * half], x[..., 2 * half:]
+    a, b = (head[..., 0::2], head[..., 1::2]) if pairs else (head[..., :half], head[..., half:])
+    u, v = a * cos - b * sin, a * sin + b * cos
+    return torch.cat((torch.stack((u, v), dim=-1).flatten(-2) if pairs else torch.cat((u, v), dim=-1), rest), dim=-1)
+
+
+def _append(s, c):
+    H, H_kv, d_h, page, dt = c["H"], c["H_kv"], c["d_h"], c["page"], DTYPES[c["dtype"]]
+    q, k, v = s["new"]
+    N = q.shape[0]
+    seq, pos = _rows(s, N)
+    angles = None if s["rope"] is None else s["rope"][pos]
+    s["out"].copy_(_rotated(_normed(q.float().view(N, H, d_h), s["norm"][0]), angles, c["pairs"]).view(N, H * d_h).to(dt))
+    key = _rotated(_normed(k.float().view(N, H_kv, d_h), s["norm"][1]), angles, c["pairs"]).to(dt)
+    to, slot = s["table"][seq, pos // page].long(), pos % page
+    s["K"][to, :, slot] = key
+    s["V"][to, :, slot] = v.view(N, H_kv, d_h)
+    # bounds: a page that gets its first token starts anew
+    fresh = torch.zeros(s["K"].shape[0], dtype=torch.bool, device="cuda")
+    fresh[to[slot == 0]] = True
+    low = s["bounds"][:, :, 0].float().masked_fill(fresh[:, None, None], math.inf)
+    high = s["bounds"][:, :, 1].float().masked_fill(fresh[:, None, None], -math.inf)
+    low.index_reduce_(0, to, key.float(), "amin")
+    high.index_reduce_(0, to, key.float(), "amax")
+    s["bounds"].copy_(torch.stack((low, high), dim=2).to(dt))
+    return dict(q=s["out"], K=s["K"], V=s["V"], bounds=s["bounds"])
+
+
+def _attend(s, c):
+    B, H, H_kv, d_h, page, dt = c["B"], c["H"], c["H_kv"], c["d_h"], c["page"], DTYPES[c["dtype"]]
+    N, G, wide = s["Q"].shape[0], H // H_kv, s["longest"]
+    seq, pos = _rows(s, N)
+    L = s["table"].shape[1] * page
+    total = s["past"].long() + (s["start"][1:] - s["start"][:-1]).long()
+    held = s["table"].long().clamp(min=0)
+    there = torch.arange(L, device="cuda") < total[:, None]                                     # [B, L]
+    keys = s["K"][held].float().permute(0, 2, 4, 1, 3).reshape(B * H_kv, d_h, L)
+    vals = s["V"][held].float().permute(0, 2, 1, 3, 4).reshape(B, H_kv, L, d_h).mul(there[:, None, :, None]).view(B * H_kv, L, d_h)
+    inside = torch.arange(N, device="cuda") - s["start"].long()[seq]
+    q = torch.zeros(B, wide, H, d_h, device="cuda")
+    q[seq, inside] = s["Q"].float().view(N, H, d_h) / math.sqrt(d_h)
+    q = q.view(B, wide, H_kv, G, d_h).permute(0, 2, 1, 3, 4).reshape(B * H_kv, wide * G, d_h)
+    score = torch.bmm(q, keys).view(B, H_kv, wide, G, L)
+    see = there[:, None, :]
+    if c["causal"]:
+        see = see & (torch.arange(L, device="cuda") <= s["past"].long()[:, None, None] + torch.arange(wide, device="cuda")[:, None])
+    score.masked_fill_(~see[:, None, :, None, :], -math.inf)
+    score.sub_(score.amax(-1, keepdim=True)).exp_()
+    weight = score.sum(-1, keepdim=True)
+    out = torch.bmm(score.view(B * H_kv, wide * G, L), vals).view(B, H_kv, wide, G, d_h) / weight
+    s["out"].copy_(out.permute(0, 2, 1, 3, 4)[seq, inside].reshape(N, H * d_h).to(dt))
+    return s["out"]
+
+
+def _select(s, c):
+    """Scores in 64 bits: the lists are decided by which of two is larger."""
+    H, H_kv, d_h, page, budget = c["H"], c["H_kv"], c["d_h"], c["page"], c["budget"]
+    N, B, P = s["Q"].shape[0], c["B"], s["table"].shape[1]
+    seq, pos = _rows(s, N)
+    bounds = s["bounds"][s["table"].long().clamp(min=0)].double().permute(0, 2, 4, 3, 1)        # [B, H_kv, d_h, 2, P]
+    q = s["Q"].double().view(N, H_kv, H // H_kv, d_h)
+    parts = torch.cat((q.clamp(max=0), q.clamp(min=0)), dim=-1)                                 # with the smallest, with the largest
+    inside, wide = torch.arange(N, device="cuda") - s["start"].long()[seq], s["longest"]
+    rows = torch.zeros(B, wide, H_kv, H // H_kv, 2 * d_h, dtype=torch.float64, device="cuda")
+    rows[seq, inside] = parts
+    score = torch.bmm(rows.permute(0, 2, 1, 3, 4).reshape(B * H_kv, -1, 2 * d_h), bounds.permute(0, 1, 3, 2, 4).reshape(B * H_kv, 2 * d_h, P))
+    score = score.view(B, H_kv, wide, H // H_kv, P).amax(3).permute(0, 2, 1, 3)[seq, inside]    # [N, H_kv, P]
+    have = pos // page + 1
+    at = torch.arange(P, device="cuda")
+    score = score.masked_fill((at < 1) | (at >= have[:, None, None] - 1), math.inf).masked_fill(at >= have[:, None, None], -math.inf)
+    order = score.sort(dim=2, descending=True, stable=True).indices
+    order = torch.nn.functional.pad(order, (0, max(0, budget - P)))[:, :, :budget]
+    count = have.clamp(max=budget)
+    none = torch.arange(budget, device="cuda") >= count[:, None, None]
+    chosen = order.masked_fill(none, P).sort(dim=2).values
+    s["lists"]["pages"].copy_(chosen.masked_fill(none, -1))
+    s["lists"]["counts"].copy_(count[:, None].expand(N, H_kv))
+    return dict(pages=s["lists"]["pages"], counts=s["lists"]["counts"])
+
+
+def _attend_pages(s, c):
+    H, H_kv, d_h, page, budget, dt = c["H"], c["H_kv"], c["d_h"], c["page"], c["budget"], DTYPES[c["dtype"]]
+    N, G = s["Q"].shape[0], H // H_kv
+    seq, pos = _rows(s, N)
+    there = torch.arange(budget, device="cuda") < s["count"][:, :, None]
+    logical = s["pages"].long().clamp(min=0)
+    at = s["table"].long()[seq[:, None, None], logical].clamp(min=0)                            # [N, H_kv, budget]
+    heads = torch.arange(H_kv, device="cuda")[:, None]
+    keys = s["K"][at, heads].float().view(N * H_kv, budget * page, d_h)
+    vals = s["V"][at, heads].float().view(N * H_kv, budget * page, d_h)
+    see = there[..., None] & (logical[..., None] * page + torch.arange(page, device="cuda") <= pos[:, None, None, None])
+    see = see.view(N * H_kv, 1, budget * page)
+    score = torch.bmm(s["Q"].float().view(N * H_kv, G, d_h) / math.sqrt(d_h), keys.transpose(1, 2).contiguous()).masked_fill_(~see, -math.inf)
+    score.sub_(score.amax(-1, keepdim=True)).exp_()
+    out = torch.bmm(score, vals * see.transpose(1, 2)) / score.sum(-1, keepdim=True)
+    s["out"].copy_(out.view(N, H * d_h).to(dt))
+    return s["out"]
+
+
+# ------------------------------------------------------------------------------------------------ what a pass needs
+def work(case):
+    """Bytes: every new row read and written once, the cache's tokens (or the pages' bounds, or the pages that the lists can name)
+    read once.  Operations: a product of d_h for every visible pair and head, twice with the values; both bounds for every page."""
+    c = case
+    new, past = _lengths(c)
+    n, esz, H, H_kv, d_h, page = sum(new), 2.0 if c["dtype"] == "bf16" else 4.0, c["H"], c["H_kv"], c["d_h"], c["page"]
+    if c["kind"] == "append":
+        return {"bytes": 2 * n * (H + 2 * H_kv) * d_h * esz + 4.0 * n * c["rot"], "flops": 6.0 * n * (H + H_kv) * d_h}
+    if c["kind"] == "attend":
+        kv = sum(a + b for a, b in zip(new, past))
+        pairs = sum(a * b + (a * (a + 1) / 2 if c["causal"] else a * a) for a, b in zip(new, past))
+        return {"bytes": 2 * n * H * d_h * esz + 2 * kv * H_kv * d_h * esz, "flops": 4.0 * H * d_h * pairs}
+    have = [[(b + i) // page + 1 for i in range(a)] for a, b in zip(new, past)]
+    if c["kind"] == "select":
+        held = sum(v[-1] for v in have)
+        return {"bytes": n * H * d_h * esz + 2 * held * H_kv * d_h * esz + 4.0 * n * H_kv * (c["budget"] + 1), "flops": 4.0 * H * d_h * sum(map(sum, have))}
+    named = [sum(min(c["budget"], x) for x in v) for v in have]
+    once = sum(min(x, v[-1]) for x, v in zip(named, have))
+    return {"bytes": 2 * n * H * d_h * esz + 2 * once * page * H_kv * d_h * esz + 4.0 * n * H_kv * (c["budget"] + 1), "flops": 4.0 * H * d_h * page * sum(named)}
+
+
+# ------------------------------------------------------------------------------------------------ in 64 bits, from the definitions
+def exact(case, seed):
+    s, c = prepare(case, seed), case
+    table, past, start = s["table"].tolist(), s["past"].tolist(), s["start"].tolist()
+    return {"append": _exact_append, "attend": _exact_attend, "select": _exact_select, "pages": _exact_pages}[c["kind"]](s, c, table, past, start)
+
+
+def _exact_head(x, w, angles, pairs):
+    """One row of heads [heads, d_h] in 64 bits: norm, then every pair as a complex number times one of modulus 1."""
+    if w is not None:
+        x = x / (x.pow(2).sum(-1, keepdim=True) / x.shape[-1] + EPS).sqrt() * w.double()
+    if angles is None:
+        return x
+    half = angles.shape[0]
+    first = torch.arange(half, device=x.device) * (2 if pairs else 1)
+    second = first + (1 if pairs else half)
+    z = torch.complex(x[:, first], x[:, second]) * torch.complex(angles[:, 0], angles[:, 1])
+    x = x.clone()
+    x[:, first], x[:, second] = z.real, z.imag
+    return x
+
+
+def _exact_append(s, c, table, past, start):
+    d_h, page = c["d_h"], c["page"]
+    q, k, v = (x.double().unflatten(1, (-1, d_h)) for x in s["new"])
+    out, K, V, bounds = torch.zeros_like(q), s["K"].double(), s["V"].double(), s["bounds"].double()
+    for b in range(c["B"]):
+        for i in range(start[b + 1] - start[b]):
+            row, p = start[b] + i, past[b] + i
+            angles = None if s["rope"] is None else s["rope"][p].double()
+            out[row] = _exact_head(q[row], s["norm"][0], angles, c["pairs"])
+            to, slot = table[b][p // page], p % page
+            key = _exact_head(k[row], s["norm"][1], angles, c["pairs"])
+            K[to, :, slot], V[to, :, slot] = key, v[row]
+            bounds[to, :, 0] = key if slot == 0 else torch.minimum(bounds[to, :, 0], key)
+            bounds[to, :, 1] = key if slot == 0 else torch.maximum(bounds[to, :, 1], key)
+    return dict(q=out.flatten(1), K=K, V=V, bounds=bounds)
+
+
+def _exact_attend(s, c, table, past, start):
+    H, H_kv, d_h, page = c["H"], c["H_kv"], c["d_h"], c["page"]
+    out = torch.zeros(s["Q"].shape[0], H, d_h, dtype=torch.float64, device="cuda")
+    for b in range(c["B"]):
+        n = start[b + 1] - start[b]
+        own_pages = torch.tensor(table[b][:-(-(past[b] + n) // page)], device="cuda")
+        for h in range(H):
+            keys = s["K"][own_pages, h // (H // H_kv)].double().flatten(0, 1)[:past[b] + n]
+            vals = s["V"][own_pages, h // (H // H_kv)].double().flatten(0, 1)[:past[b] + n]
+            logits = s["Q"][start[b]:start[b + 1], h * d_h:(h + 1) * d_h].double() @ keys.t().contiguous() * d_h ** -0.5
+            if c["causal"]:
+                logits += torch.full_like(logits, -math.inf).triu_(past[b] + 1)
+            out[start[b]:start[b + 1], h] = torch.softmax(logits, dim=1) @ vals
+    return out.flatten(1)
+
+
+def _exact_select(s, c, table, past, start):
+    H_kv, G, d_h, page, budget = c["H_kv"], c["H"] // c["H_kv"], c["d_h"], c["page"], c["budget"]
+    N = s["Q"].shape[0]
+    pages, counts = torch.full((N, H_kv, budget), -1, dtype=torch.int32), torch.zeros(N, H_kv, dtype=torch.int32)
+    for b in range(c["B"]):
+        n = start[b + 1] - start[b]
+        bounds = s["bounds"][torch.tensor(table[b][:-(-(past[b] + n) // page)], device="cuda")].double()
+        for h in range(H_kv):
+            low, high = bounds[:, h, 0], bounds[:, h, 1]
+            for i0 in range(0, n, 64):
+                q = s["Q"][start[b] + i0:min(start[b] + i0 + 64, start[b + 1])].double().view(-1, H_kv, G, 1, d_h)[:, h]
+                score = torch.maximum(q * low, q * high).sum(-1).amax(1).cpu()
+                for i in range(score.shape[0]):
+                    have = (past[b] + i0 + i) // page + 1
+                    free = sorted(range(1, have - 1), key=lambda j: (-float(score[i, j]), j)) if have > budget else list(range(1, have - 1))
+                    chosen = sorted({0, have - 1} | set(free[:budget - 2]))
+                    pages[start[b] + i0 + i, h, :len(chosen)] = torch.tensor(chosen, dtype=torch.int32)
+                    counts[start[b] + i0 + i, h] = len(chosen)
+    return dict(pages=pages.cuda(), counts=counts.cuda())
+
+
+def _exact_pages(s, c, table, past, start):
+    H_kv, G, d_h, page = c["H_kv"], c["H"] // c["H_kv"], c["d_h"], c["page"]
+    out = torch.zeros(s["Q"].shape[0], H_kv, G, d_h, dtype=torch.float64, device="cuda")
+    for b in range(c["B"]):
+        numbers = torch.tensor(table[b], device="cuda")
+        for row in range(start[b], start[b + 1]):
+            p = past[b] + row - start[b]
+            k = int(s["count"][row, 0])
+            listed_pages = s["pages"][row, :, :k].long()                                        # [H_kv, k]
+            at = listed_pages[:, :, None] * page + torch.arange(page, device="cuda")
+            heads = torch.arange(H_kv, device="cuda")[:, None]
+            keys = s["K"][numbers[listed_pages].long(), heads].double().flatten(1, 2)
+            vals = s["V"][numbers[listed_pages].long(), heads].double().flatten(1, 2)
+            logits = torch.bmm(s["Q"][row].double().view(H_kv, G, d_h), keys.transpose(1, 2).contiguous()) * d_h ** -0.5
+            logits = logits.masked_fill((at.flatten(1) > p)[:, None], -math.inf)
+            out[row] = torch.bmm(torch.softmax(logits, dim=2), vals)
+    return out.flatten(1)
