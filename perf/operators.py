@@ -252,7 +252,7 @@ def _attend(s, c):
     held = s["table"].long().clamp(min=0)
     there = torch.arange(L, device="cuda") < total[:, None]                                     # [B, L]
     keys = s["K"][held].float().permute(0, 2, 4, 1, 3).reshape(B * H_kv, d_h, L)
-    vals = s["V"][held].float().permute(0, 2, 1, 3, 4).reshape(B, H_kv, L, d_h).mul(there[:, None, :, None]).view(B * H_kv, L, d_h)
+    vals = s["V"][held].float().permute(0, 2, 1, 3, 4).reshape(B, H_kv, L, d_h).mul(there[:, None, :, None]).reshape(B * H_kv, L, d_h)
     inside = torch.arange(N, device="cuda") - s["start"].long()[seq]
     q = torch.zeros(B, wide, H, d_h, device="cuda")
     q[seq, inside] = s["Q"].float().view(N, H, d_h) / math.sqrt(d_h)
@@ -303,8 +303,8 @@ def _attend_pages(s, c):
     logical = s["pages"].long().clamp(min=0)
     at = s["table"].long()[seq[:, None, None], logical].clamp(min=0)                            # [N, H_kv, budget]
     heads = torch.arange(H_kv, device="cuda")[:, None]
-    keys = s["K"][at, heads].float().view(N * H_kv, budget * page, d_h)
-    vals = s["V"][at, heads].float().view(N * H_kv, budget * page, d_h)
+    keys = s["K"][at, heads].float().reshape(N * H_kv, budget * page, d_h)
+    vals = s["V"][at, heads].float().reshape(N * H_kv, budget * page, d_h)
     see = there[..., None] & (logical[..., None] * page + torch.arange(page, device="cuda") <= pos[:, None, None, None])
     see = see.view(N * H_kv, 1, budget * page)
     score = torch.bmm(s["Q"].float().view(N * H_kv, G, d_h) / math.sqrt(d_h), keys.transpose(1, 2).contiguous()).masked_fill_(~see, -math.inf)
