@@ -364,6 +364,117 @@ int ada_cascade_layers_adaptive(const void* const* X_layers, int L, int T, int d
                                 void* ws, size_t ws_bytes, void* stream, unsigned flags);
 
 /*
+ * A paged cache of keys and values, and attention over it: what a program that serves a model keeps from call to call, and
+ * what its new tokens read.  The calls above take the Q, K and V of a whole prompt; these take the new tokens of several
+ * sequences and find everything else in the cache.
+ *
+ * A page holds `page` consecutive tokens of one sequence.  Element (page, head, slot, i) of K and of V lies at
+ * page * page_stride + head * head_stride + slot * slot_stride + i: [pages][H_kv][page][d_h] reads fastest (a page of a head is one
+ * piece of memory), token by token with heads side by side works as well.
+ * bounds: [pages][H_kv][2][d_h], the smallest and the largest value of every column over the page's keys, which ada_cache_append
+ * keeps and ada_select_pages reads.  NULL where no pages are selected.
+ */
+typedef struct {
+    void* K;
+    void* V;
+    void* bounds;           /* or NULL */
+    int pages;              /* pages in the pool */
+    int page;               /* tokens per page: 16, 32, 64, 128 or 256 */
+    int H_kv;               /* heads of keys and values */
+    int d_h;                /* 64, 128 or, for bf16, 256 */
+    int dtype;
+    int64_t page_stride;    /* elements; strides in whole 16-byte pieces, K, V and bounds 16-byte aligned */
+    int64_t head_stride;
+    int64_t slot_stride;
+} ada_paged_cache;
+
+/*
+ * The new tokens of B sequences.  All arrays are DEVICE memory, so that a captured graph serves the next step too.
+ *   table  [B][table_stride] int32   sequence b's token at position p lies in page table[b][p / page] (entries behind its last
+ *                                    page are not read)
+ *   start  [B + 1] int32             sequence b's new tokens are rows start[b] .. start[b + 1] - 1 of Q (and K, V, the outputs);
+ *                                    rows from start[B] on belong to nobody and are left as they are
+ *   past   [B] int32                 its tokens in front of these: row start[b] + i is position past[b] + i
+ */
+typedef struct {
+    int B;                  /* 1 .. ADA_MAX_BATCH */
+    int rows;               /* rows of Q and of the outputs, at least start[B] */
+    int longest;            /* no sequence has more new tokens than this */
+    int max_pages;          /* entries of a row of table */
+    const int32_t* table;
+    int64_t table_stride;   /* >= max_pages (any for B = 1) */
+    const int32_t* start;
+    const int32_t* past;
+} ada_paged_chunk;
+
+/*
+ * status [1] int32 (device) of the four calls below: what the host cannot see.  It is only ever raised, never cleared, so one word
+ * serves many calls; zero it before the first.
+ *   ADA_ERR_INDEX   a page number outside the pool, a position behind the rope table, an entry of a page list that is out of range or not larger than the
+ *                   one in front of it.  Nothing is read or written there: a token without a page is not appended, keys without one count as masked
+ *   ADA_ERR_SHAPE   a sequence whose start descends, leaves the rows or exceeds `longest`, whose past is negative or whose tokens do not fit into
+ *                   max_pages pages: its rows are not written.  (The larger code wins where both occur.)
+ * Two sequences may share pages that are only read.  A page that a call appends to belongs to one sequence.
+ */
+
+/* Bytes of workspace that ada_attention_paged and ada_attention_pages need for these sizes (256-byte aligned); it need not be
+ * cleared.  0 for arguments that those calls refuse. */
+size_t ada_paged_workspace_bytes(const ada_paged_cache* cache, const ada_paged_chunk* chunk, int H);
+
+/*
+ * Appends the new tokens' keys and values and rotates their queries.  Per head h and row t at position p
+ *   q' = Rot_p(q / sqrt(mean(q^2) + eps) * q_norm),  k' = Rot_p(k / sqrt(mean(k^2) + eps) * k_norm)
+ * in fp32, rounded once; q' goes to q_out, k' and v to the cache, and the page's bounds are widened by k' (a page's first slot starts
+ * them anew).  Rot_p turns the pairs (i, i + rot / 2) of the first `rot` columns, or (2 i, 2 i + 1) with ADA_FLAG_ROPE_PAIRS, by the angle whose
+ * cosine and sine are rope[p][i]: (a, b) -> (a cos - b sin, a sin + b cos).
+ *   Q, K, V   rows x (H d_h), rows x (H_kv d_h) twice, leading dimensions ldq, ldk, ldv; 16-byte aligned rows (views into one
+ *             projection's output are fine).  Q and q_out may be NULL (keys and values only)
+ *   q_norm, k_norm   [d_h] in the cache's dtype, or NULL: no norm of that side
+ *   rope      [rope_len][rot / 2][2] float, or NULL: no rotation.  rot: a multiple of 16, at most d_h
+ *   q_out     rows x (H d_h) in the cache's dtype; may be Q itself
+ */
+#define ADA_FLAG_ROPE_PAIRS 32u
+int ada_cache_append(const ada_paged_cache* cache, const ada_paged_chunk* chunk, const void* Q, int64_t ldq,
+                     const void* K, int64_t ldk, const void* V, int64_t ldv, int H,
+                     const void* q_norm, const void* k_norm, float eps, const float* rope, int rot, int rope_len,
+                     void* q_out, int64_t ldq_out, int32_t* status, void* stream, unsigned flags);
+
+/*
+ * Attention of the new tokens over the cache (their own keys and values appended already):
+ *   out[t, h] = softmax over s of (q_t . k_s / sqrt(d_h)) v_s,  s over all tokens of t's sequence (past and new), with
+ * ADA_FLAG_ATTN_CAUSAL over those not later than t.  Query head h reads head h / (H / H_kv) of the cache; H is a multiple of H_kv.
+ * Chunks and single tokens, in any mixture.
+ *   Q     rows x (H d_h), the cache's dtype, leading dimension ldq, 16-byte aligned rows
+ *   out   rows x (H d_h), the cache's dtype, leading dimension ld_out, 16-byte aligned rows.  A row that sees no key is 0
+ * Sums, maxima and (fp32 caches) all products in fp32.  What lies behind a sequence's last token is never read.
+ */
+int ada_attention_paged(const ada_paged_cache* cache, const ada_paged_chunk* chunk, const void* Q, int H, int64_t ldq,
+                        void* out, int64_t ld_out, int32_t* status, void* ws, size_t ws_bytes, void* stream, unsigned flags);
+
+/*
+ * Which pages a new token attends to: for every row t and head of the cache the pages with the largest scores
+ *   score(page) = max over the query heads h of the group of  sum_i max(q_i lo_i, q_i hi_i)
+ * with lo, hi the page's bounds: no key of the page has a larger product with q.  Which pages those are is decided as in float64, ties go to the
+ * smaller number.
+ *   budget       pages per row and head, 1 .. max_pages (or more)
+ *   first, last  the first and the last so many pages that a row sees are chosen whatever they score (first + last <= budget)
+ *   pages  [rows][H_kv][budget] int32   page numbers within the sequence (0 = its first), ascending, -1 behind the last chosen one
+ *   counts [rows][H_kv] int32           how many
+ * A row sees the pages of its sequence, with ADA_FLAG_ATTN_CAUSAL up to the one it lies in.  max_pages <= ADA_SELECT_MAX_PAGES.
+ */
+#define ADA_SELECT_MAX_PAGES 8192
+int ada_select_pages(const ada_paged_cache* cache, const ada_paged_chunk* chunk, const void* Q, int H, int64_t ldq,
+                     int budget, int first, int last, int32_t* pages, int32_t* counts, int32_t* status, void* stream, unsigned flags);
+
+/*
+ * ada_attention_paged with s in the pages that are listed for the row and its head of the cache only (ada_select_pages' outputs, or any
+ * strictly ascending list).  A list's entries from counts on are not read.
+ */
+int ada_attention_pages(const ada_paged_cache* cache, const ada_paged_chunk* chunk, const void* Q, int H, int64_t ldq,
+                        const int32_t* pages, const int32_t* counts, int budget,
+                        void* out, int64_t ld_out, int32_t* status, void* ws, size_t ws_bytes, void* stream, unsigned flags);
+
+/*
  * Which tile shape a one-launch cascade step takes when `workgroups` workgroups share its tiles (the CU count for a
  * single problem; that divided by the number of groups for a grouped call) and the rows come in whole aligned
  * 128-byte chunks of bf16: 0 = 64 x 64 (in quarters where d <= 1024 and each of those has a workgroup of its own),

@@ -6,9 +6,11 @@ result to the host and raises on a device-reported status.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import subprocess
+import tempfile
 from typing import Dict, List, Optional, Sequence
 
 import torch
@@ -16,7 +18,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libada.so")
 SRC_DIR = os.path.join(_HERE, "csrc")
-SOURCES = ("ada_kernels.hip",)
+SOURCES = ("ada_kernels.hip", "ada_paged.hip")
 
 ADA_F32, ADA_BF16 = 0, 1
 FLAG_CROSS_EARLIER_ONLY = 1
@@ -24,13 +26,16 @@ FLAG_TWO_PASS = 2
 FLAG_RESIDENT_PASS = 4
 FLAG_ATTN_CAUSAL = 8
 FLAG_GREEDY_COVER = 16
+FLAG_ROPE_PAIRS = 32
+SELECT_MAX_PAGES = 8192
 OK = 0
 
 SYMBOLS = ("ada_status_string", "ada_workspace_bytes", "ada_workspace_zero_bytes", "ada_workspace_init", "ada_select_full", "ada_cascade_step",
            "ada_cascade_layers", "ada_cascade_layers_batched", "ada_cascade_step_grouped", "ada_cascade_layers_grouped", "ada_select_full_grouped", "ada_pipeline_layers", "ada_cascade_layers_adaptive", "ada_plan_tile_shape", "ada_plan_full_units",
            "ada_set_overlap", "ada_cascade_report", "ada_profile_enable",
            "ada_profile_collect", "ada_profile_copy_probe", "ada_profile_mfma_probe", "ada_assign_nearest",
-           "ada_attention_compressed", "ada_cascade_step_static")
+           "ada_attention_compressed", "ada_cascade_step_static", "ada_paged_workspace_bytes", "ada_cache_append", "ada_attention_paged",
+           "ada_select_pages", "ada_attention_pages")
 
 KERNEL_CLASSES = ("norm_prep", "gram_full", "gram_rep", "gram_cross", "update", "cascade_fused", "mfma_probe", "assign", "attn", "screen")
 
@@ -45,6 +50,19 @@ class AdaTauControl(ctypes.Structure):
     """ada_tau_control of include/ada.h."""
     _fields_ = [("kappa", ctypes.c_double), ("eta_target", ctypes.c_double), ("tau_min", ctypes.c_double),
                 ("tau_max", ctypes.c_double)]
+
+
+class AdaPagedCache(ctypes.Structure):
+    """ada_paged_cache of include/ada.h."""
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("bounds", ctypes.c_void_p), ("pages", ctypes.c_int),
+                ("page", ctypes.c_int), ("H_kv", ctypes.c_int), ("d_h", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64)]
+
+
+class AdaPagedChunk(ctypes.Structure):
+    """ada_paged_chunk of include/ada.h."""
+    _fields_ = [("B", ctypes.c_int), ("rows", ctypes.c_int), ("longest", ctypes.c_int), ("max_pages", ctypes.c_int),
+                ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("start", ctypes.c_void_p), ("past", ctypes.c_void_p)]
 
 
 class AdaError(RuntimeError):
@@ -80,6 +98,11 @@ SCRATCH_BUDGET = {
     "k_attn_rep2ILi128E": 0,
     "k_attn_rep2ILi64E": 0,
     "k_attn_repIfL": 0,                        # and in fp32
+    "k_paged_rowsI": 0,                        # the paged cache
+    "k_paged_joinI": 0,
+    "k_cache_appendI": 0,
+    "k_cache_boundsI": 0,
+    "k_select_pagesI": 0,
 }
 
 
@@ -103,15 +126,23 @@ def build_library(verbose: bool = False) -> str:
     """Compile the HIP sources for gfx950 into libada.so next to this file; fails if a hot kernel needs more private
     memory than SCRATCH_BUDGET allows."""
     tmp = LIB_PATH + ".tmp.%d" % os.getpid()
-    cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Rpass-analysis=kernel-resource-usage"]
-    cmd += [os.path.join(SRC_DIR, s) for s in SOURCES] + ["-o", tmp]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
-    if verbose:
-        print(res.stderr)
-    usage = kernel_resources(res.stderr)
+    flags = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Rpass-analysis=kernel-resource-usage"]
+    usage: Dict[str, Dict[str, int]] = {}
+    with tempfile.TemporaryDirectory() as objects:                 # the sources side by side
+        parts = [os.path.join(objects, s + ".o") for s in SOURCES]
+        runs = [subprocess.Popen(flags + ["-c", os.path.join(SRC_DIR, s), "-o", o], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+                for s, o in zip(SOURCES, parts)]
+        said = [r.communicate()[0] for r in runs]
+        for r, text in zip(runs, said):
+            if r.returncode != 0:
+                raise RuntimeError("hipcc failed:\n" + text)
+            if verbose:
+                print(text)
+            usage.update(kernel_resources(text))
+        res = subprocess.run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC"] + parts + ["-o", tmp], capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
     for tag, budget in SCRATCH_BUDGET.items():
         hits = {k: v for k, v in usage.items() if tag in k}
         if not hits:
@@ -202,6 +233,17 @@ def lib():
         L.ada_attention_compressed.restype = i32
         L.ada_attention_compressed.argtypes = [vp, vp, vp, i32, i32, i32, i64, i32, vp, i32, vp, vp, vp, i64, vp,
                                                vp, sz, vp, u32]
+        cp, kp = ctypes.POINTER(AdaPagedCache), ctypes.POINTER(AdaPagedChunk)
+        L.ada_paged_workspace_bytes.restype = sz
+        L.ada_paged_workspace_bytes.argtypes = [cp, kp, i32]
+        L.ada_cache_append.restype = i32
+        L.ada_cache_append.argtypes = [cp, kp, vp, i64, vp, i64, vp, i64, i32, vp, vp, f32, vp, i32, i32, vp, i64, vp, vp, u32]
+        L.ada_attention_paged.restype = i32
+        L.ada_attention_paged.argtypes = [cp, kp, vp, i32, i64, vp, i64, vp, vp, sz, vp, u32]
+        L.ada_select_pages.restype = i32
+        L.ada_select_pages.argtypes = [cp, kp, vp, i32, i64, i32, i32, i32, vp, vp, vp, vp, u32]
+        L.ada_attention_pages.restype = i32
+        L.ada_attention_pages.argtypes = [cp, kp, vp, i32, i64, vp, vp, i32, vp, i64, vp, vp, sz, vp, u32]
         L.ada_assign_nearest.restype = i32
         L.ada_assign_nearest.argtypes = [vp, i32, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp, u32]
         _lib = L
@@ -673,6 +715,188 @@ def ada_cascade_layers_adaptive(Xs: Sequence[torch.Tensor], tau0: float, kappa: 
         raise AdaError(rc, "ada_cascade_layers_adaptive")
     out["_keep"] = (ws, list(Xs))
     return out
+
+
+class PagedCache:
+    """A paged cache: K, V [pages, H_kv, page, d_h] of one dtype, device and strides (views of any order with unit stride along d_h; head by
+    head, as the shape says, reads fastest); bounds [pages, H_kv, 2, d_h], contiguous: smallest and largest key of every page by columns, for the
+    selection of pages, or None.  Holds the tensors and their description; making one costs no GPU work."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, bounds: Optional[torch.Tensor] = None):
+        if not K.is_cuda or K.dim() != 4 or K.stride(3) != 1:
+            raise ValueError("K must be a [pages, H_kv, page, d_h] device tensor with unit stride along d_h")
+        if V.shape != K.shape or V.dtype != K.dtype or V.device != K.device or V.stride() != K.stride():
+            raise ValueError("K and V must share shape, dtype, device and strides")
+        pages, H_kv, page, d_h = K.shape
+        if bounds is not None and (tuple(bounds.shape) != (pages, H_kv, 2, d_h) or bounds.dtype != K.dtype or bounds.device != K.device
+                                   or not bounds.is_contiguous()):
+            raise ValueError("bounds must be a contiguous [pages, H_kv, 2, d_h] tensor like K")
+        self.K, self.V, self.bounds = K, V, bounds
+        self.pages, self.H_kv, self.page, self.d_h = pages, H_kv, page, d_h
+        # (a dimension of one element steps nowhere: its stride is torch's to choose)
+        self.desc = AdaPagedCache(_ptr(K), _ptr(V), _ptr(bounds), pages, page, H_kv, d_h, _dtype_code(K),
+                                  K.stride(0) if pages > 1 else K.stride(2) * page, K.stride(1) if H_kv > 1 else K.stride(2) * page, K.stride(2))
+        self.ref = ctypes.byref(self.desc)
+
+
+class Chunk:
+    """The new tokens of several sequences: table [B, max_pages], start [B + 1], past [B] (int32 device tensors), `rows` rows of new
+    tokens in all (at least start[B]), no sequence with more than `longest` (None: rows) of them.  include/ada.h has the details."""
+
+    def __init__(self, table: torch.Tensor, start: torch.Tensor, past: torch.Tensor, *, rows: int, longest: Optional[int] = None):
+        B = past.numel()
+        for t, name in ((table, "table"), (start, "start"), (past, "past")):
+            if t.dtype != torch.int32 or not t.is_cuda or t.device != table.device:
+                raise ValueError("%s must be an int32 device tensor" % name)
+        if table.dim() != 2 or table.shape[0] != B or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table must be [B, max_pages] with contiguous rows")
+        if start.dim() != 1 or past.dim() != 1 or start.numel() != B + 1 or not start.is_contiguous() or not past.is_contiguous():
+            raise ValueError("start must be [B + 1] and past [B], both contiguous")
+        self.table, self.start, self.past, self.B, self.rows = table, start, past, B, int(rows)
+        self.desc = AdaPagedChunk(B, self.rows, self.rows if longest is None else int(longest), table.shape[1], _ptr(table),
+                                  table.stride(0) if B > 1 else table.shape[1], _ptr(start), _ptr(past))
+        self.ref = ctypes.byref(self.desc)
+
+
+def ada_paged_workspace_bytes(cache: PagedCache, chunk: Chunk, H: int) -> int:
+    return int(lib().ada_paged_workspace_bytes(cache.ref, chunk.ref, int(H)))
+
+
+def paged_workspace(cache: PagedCache, chunk: Chunk, H: int) -> torch.Tensor:
+    """A workspace for ada_attention_paged and ada_attention_pages of these sizes (it holds nothing between calls)."""
+    n = ada_paged_workspace_bytes(cache, chunk, H)
+    if n == 0:
+        raise ValueError("sizes that no paged attention takes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.K.device)
+
+
+def _paged_rows(cache: PagedCache, chunk: Chunk, X: torch.Tensor, name: str, heads: Optional[int] = None) -> int:
+    """The heads of rows x (heads * d_h)."""
+    if X.dim() != 2 or X.dtype != cache.K.dtype or X.device != cache.K.device or (X.shape[1] > 1 and X.stride(1) != 1):
+        raise ValueError("%s must be a rows x (heads * d_h) tensor of the cache's dtype and device with unit column stride" % name)
+    n = X.shape[1] // cache.d_h
+    if X.shape[0] < chunk.rows or n * cache.d_h != X.shape[1] or (heads is not None and n != heads):
+        raise ValueError("%s must have %d rows (or more) and %s heads of %d" % (name, chunk.rows, "some" if heads is None else heads, cache.d_h))
+    return n
+
+
+def _paged_status(cache: PagedCache, status: Optional[torch.Tensor]) -> torch.Tensor:
+    if status is None:
+        return torch.zeros(1, dtype=torch.int32, device=cache.K.device)
+    if status.dtype != torch.int32 or status.device != cache.K.device or status.numel() < 1:
+        raise ValueError("status must be an int32 tensor on the cache's device")
+    return status
+
+
+def _ld(X: torch.Tensor) -> int:
+    return X.stride(0) if X.shape[0] > 1 else X.shape[1]       # (one row steps nowhere)
+
+
+def _on(cache: PagedCache, chunk: Chunk):
+    """The cache's device as the current one, for calls made beside another."""
+    if chunk.table.device != cache.K.device:
+        raise ValueError("cache and chunk must share their device")
+    return torch.cuda.device(cache.K.device) if cache.K.device.index != torch._C._cuda_getDevice() else contextlib.nullcontext()
+
+
+def ada_cache_append(cache: PagedCache, chunk: Chunk, Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, *,
+                     rope: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None,
+                     eps: float = 1e-6, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None,
+                     flags: int = 0) -> Dict[str, torch.Tensor]:
+    """Norm per head, rotation, and the new tokens' keys and values into the cache (its bounds widened where it has them).  Q, K, V: rows x
+    (heads * d_h), views of one projection's output if need be; Q may be None.  rope: [positions, rot / 2, 2] float32 cosines and sines; q_norm,
+    k_norm: [d_h] weights or None.  Returns q (`out` if given; may be Q) and status, an int32 word that errors raise."""
+    H = None if Q is None else _paged_rows(cache, chunk, Q, "Q")
+    _paged_rows(cache, chunk, K, "K", cache.H_kv)
+    _paged_rows(cache, chunk, V, "V", cache.H_kv)
+    for w, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if w is not None and (tuple(w.shape) != (cache.d_h,) or w.dtype != K.dtype or w.device != K.device or not w.is_contiguous()):
+            raise ValueError("%s must be a contiguous [d_h] tensor like K" % name)
+    if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2 or rope.dtype != torch.float32 or rope.device != K.device or not rope.is_contiguous()):
+        raise ValueError("rope must be a contiguous float32 [positions, rot / 2, 2] device tensor")
+    status = _paged_status(cache, status)
+    if Q is None:
+        out = None
+    elif out is None:
+        out = torch.empty((Q.shape[0], Q.shape[1]), dtype=Q.dtype, device=Q.device)
+    else:
+        _paged_rows(cache, chunk, out, "out", H)
+    with _on(cache, chunk):
+        rc = lib().ada_cache_append(cache.ref, chunk.ref, _ptr(Q), 0 if Q is None else _ld(Q), _ptr(K), _ld(K), _ptr(V), _ld(V),
+                                    cache.H_kv if H is None else H, _ptr(q_norm), _ptr(k_norm), float(eps), _ptr(rope),
+                                    0 if rope is None else 2 * rope.shape[1], 0 if rope is None else rope.shape[0], _ptr(out),
+                                    0 if out is None else _ld(out), _ptr(status), _stream(stream), int(flags))
+    if rc != OK:
+        raise AdaError(rc, "ada_cache_append")
+    return dict(q=out, status=status, _keep=(cache, chunk, Q, K, V, rope, q_norm, k_norm))
+
+
+def _paged_attention(cache, chunk, Q, lists, ws, out, status, stream, flags, name):
+    H = _paged_rows(cache, chunk, Q, "Q")
+    status = _paged_status(cache, status)
+    ws = paged_workspace(cache, chunk, H) if ws is None else ws
+    if out is None:
+        out = torch.empty((Q.shape[0], Q.shape[1]), dtype=Q.dtype, device=Q.device)
+    else:
+        _paged_rows(cache, chunk, out, "out", H)
+    with _on(cache, chunk):
+        if lists is None:
+            rc = lib().ada_attention_paged(cache.ref, chunk.ref, _ptr(Q), H, _ld(Q), _ptr(out), _ld(out), _ptr(status), _ptr(ws), ws.numel(),
+                                           _stream(stream), int(flags))
+        else:
+            rc = lib().ada_attention_pages(cache.ref, chunk.ref, _ptr(Q), H, _ld(Q), _ptr(lists[0]), _ptr(lists[1]), lists[0].shape[2], _ptr(out),
+                                           _ld(out), _ptr(status), _ptr(ws), ws.numel(), _stream(stream), int(flags))
+    if rc != OK:
+        raise AdaError(rc, name)
+    return dict(out=out, status=status, _keep=(cache, chunk, Q, lists, ws))
+
+
+def ada_attention_paged(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, *, ws: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None,
+                        flags: int = 0) -> Dict[str, torch.Tensor]:
+    """Attention of the new tokens over everything their sequences have in the cache (FLAG_ATTN_CAUSAL: up to themselves).  Q: rows x
+    (H * d_h), H a multiple of the cache's heads.  Returns out (like Q) and status, an int32 word that errors raise."""
+    return _paged_attention(cache, chunk, Q, None, ws, out, status, stream, flags, "ada_attention_paged")
+
+
+def _check_lists(cache, chunk, pages, counts):
+    if pages.dtype != torch.int32 or pages.dim() != 3 or pages.shape[0] < chunk.rows or pages.shape[1] != cache.H_kv or not pages.is_contiguous() \
+            or pages.device != cache.K.device:
+        raise ValueError("pages must be a contiguous [rows, H_kv, budget] int32 tensor on the cache's device")
+    if counts.dtype != torch.int32 or tuple(counts.shape) != tuple(pages.shape[:2]) or not counts.is_contiguous() or counts.device != pages.device:
+        raise ValueError("counts must be a contiguous [rows, H_kv] int32 tensor beside pages")
+
+
+def ada_select_pages(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, budget: int, *, first: int = 1, last: int = 1,
+                     out: Optional[Dict[str, torch.Tensor]] = None, ws: Optional[torch.Tensor] = None,
+                     status: Optional[torch.Tensor] = None, stream=None, flags: int = 0) -> Dict[str, torch.Tensor]:
+    """For every row and head of the cache the `budget` pages of its sequence that its queries may weigh most, by the pages' bounds; the
+    `first` and `last` pages it sees are always among them.  Returns pages [rows, H_kv, budget] int32 (ascending, -1 behind the last), counts
+    [rows, H_kv] int32 (`out`'s, if given) and status.  No workspace is needed; `ws` is taken so that the paged calls look alike."""
+    H = _paged_rows(cache, chunk, Q, "Q")
+    if cache.bounds is None:
+        raise ValueError("the cache has no bounds to score pages by")
+    status = _paged_status(cache, status)
+    if out is None:
+        out = dict(pages=torch.empty((chunk.rows, cache.H_kv, int(budget)), dtype=torch.int32, device=Q.device),
+                   counts=torch.empty((chunk.rows, cache.H_kv), dtype=torch.int32, device=Q.device))
+    _check_lists(cache, chunk, out["pages"], out["counts"])
+    if out["pages"].shape[2] != int(budget):
+        raise ValueError("pages must have `budget` entries per row and head")
+    with _on(cache, chunk):
+        rc = lib().ada_select_pages(cache.ref, chunk.ref, _ptr(Q), H, _ld(Q), int(budget), int(first), int(last), _ptr(out["pages"]),
+                                    _ptr(out["counts"]), _ptr(status), _stream(stream), int(flags))
+    if rc != OK:
+        raise AdaError(rc, "ada_select_pages")
+    return dict(pages=out["pages"], counts=out["counts"], status=status, _keep=(cache, chunk, Q))
+
+
+def ada_attention_pages(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, pages: torch.Tensor, counts: torch.Tensor, *,
+                        ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                        stream=None, flags: int = 0) -> Dict[str, torch.Tensor]:
+    """ada_attention_paged over the listed pages only: pages [rows, H_kv, budget] and counts [rows, H_kv] as ada_select_pages leaves them."""
+    _check_lists(cache, chunk, pages, counts)
+    return _paged_attention(cache, chunk, Q, (pages, counts), ws, out, status, stream, flags, "ada_attention_pages")
 
 
 def ada_plan_tile_shape(r: int, T: int, d: int, workgroups: int) -> int:

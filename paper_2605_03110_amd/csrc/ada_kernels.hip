@@ -31,6 +31,7 @@
 #include <vector>
 
 #include "../../include/ada.h"
+#include "ada_hooks.hpp"
 
 namespace {
 
@@ -2008,6 +2009,11 @@ int run_cascade(const void* X, int T, int d, long long ld, int dtype, float tau,
 }
 
 }  // namespace
+
+// for the other translation units (ada_hooks.hpp)
+void* ada_hook_prof_open(int cls, hipStream_t st) { return g_prof_on ? new ProfScope(cls, st) : nullptr; }
+void ada_hook_prof_close(void* scope) { delete reinterpret_cast<ProfScope*>(scope); }
+int ada_hook_cus() { return device_cus(); }
 
 // ------------------------------------------------------------------------------------------------
 // C ABI

@@ -1,0 +1,549 @@
+// Attention of new tokens over a paged cache, and over listed pages of it.
+//
+// A head of the cache and up to 16 of the query rows that read it (tokens x heads of the group, flat row = token * G + head) make a tile.  Its
+// keys come in units of 128; the units of all tiles stand in one line, which is cut into as many equal pieces as there are workgroups, so
+// that one long sequence and many short ones fill the chip alike.  A piece that holds a whole tile writes the output; a tile that is cut leaves
+// rows, maxima and sums per piece, which k_paged_join puts together in the order of the keys (the same result on every run).
+//
+// Inside a unit each of the four waves takes 32 keys: S^T = K Q^T with keys straight from memory in registers (a lane's 16 bytes of one key are the operand
+// as it is), softmax over keys = registers and two lane swaps, O^T += V^T P^T with the weights as they come out of the first product.  In bf16 the values
+// pass through LDS and are read transposed; weights enter as pairs hi + lo of bf16 (2^-17 relative), which costs nothing where memory bounds.  In fp32
+// the matrix instruction takes one number per lane and the column order of O is free, so that a lane's 16 bytes of a value row serve without LDS.
+#pragma once
+
+struct AttendArgs {
+    PagedArgs p;
+    const void* Q;
+    long long ldq;
+    void* out;
+    long long ld_out;
+    float sc2;                                             // log2(e) / sqrt(d_h)
+    const int32_t *list, *count;                           // listed pages, or NULL
+    int budget;
+    const long long* prefix;                               // [tiles + 1] units in front of a tile of one head (k_paged_plan)
+    const int2* tile;                                      // [tiles] its sequence and number in it
+    const int* tiles;
+    float *part_o, *part_ml;                               // per piece two cut tiles: [16][DH] rows, [16][2] maxima and sums
+};
+
+constexpr int TILE_ROWS = 16, UNIT = 128, WAVE_KEYS = 32;
+
+// ------------------------------------------------------------------------------------------------ who does what
+// Units of every tile of one head, one workgroup.
+__global__ __launch_bounds__(1024) void k_paged_plan(PagedArgs p, int tile_rows, int unit, long long* prefix, int2* tile, int* tiles) {
+    __shared__ int base[ADA_MAX_BATCH + 1];
+    __shared__ long long sums[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // inclusive sum over the workgroup's values
+    auto scan = [&](long long v) {
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const long long u = __shfl_up(v, o, 64);
+            if (lane >= o) v += u;
+        }
+        __syncthreads();
+        if (lane == 63) sums[wave] = v;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) v += sums[w];
+        return v;
+    };
+    int carry = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 1024) {
+        const int b = b0 + tid;
+        const int mine = b < p.B ? (int)(((long long)paged_seq(p, b).n * p.G + tile_rows - 1) / tile_rows) : 0;
+        const int upto = carry + (int)scan(mine);
+        if (b < p.B) base[b + 1] = upto;
+        __syncthreads();
+        carry = base[min(b0 + 1024, p.B)];
+    }
+    if (tid == 0) base[0] = 0;
+    __syncthreads();
+    const int n_tiles = base[p.B];
+    long long front = 0;
+    for (int t0 = 0; t0 < n_tiles; t0 += 1024) {
+        const int t = t0 + tid;
+        long long mine = 0;
+        if (t < n_tiles) {
+            int lo = 0, hi = p.B;                          // the last b with base[b] <= t
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (base[mid] <= t) lo = mid; else hi = mid;
+            }
+            const int j = t - base[lo];
+            const Seq s = paged_seq(p, lo);
+            const int last = (int)min((long long)s.n - 1, ((long long)(j + 1) * tile_rows - 1) / p.G);
+            mine = ((p.causal ? s.past + last + 1 : s.len) + unit - 1) / unit;
+            tile[t] = {lo, j};
+        }
+        const long long upto = front + scan(mine);
+        if (t < n_tiles) prefix[t + 1] = upto;
+        __syncthreads();
+        if (tid == 1023) sums[0] = upto;
+        __syncthreads();
+        front = sums[0];
+        __syncthreads();
+    }
+    if (tid == 0) { prefix[0] = 0; *tiles = n_tiles; }
+}
+
+// A tile of one head, and where its units stand in the line.
+struct Tile {
+    long long at;                                          // its first unit
+    int units, kvh;
+    Seq s;
+    int b, j;                                              // rows 16 j .. of the sequence's n G, or (listed) of the token's G
+    int row;                                               // listed: the token's row
+    bool any;                                              // somebody's (listed: the row may be nobody's)
+};
+
+template <bool LISTED>
+__device__ inline long long line_length(const AttendArgs& a) {
+    if (LISTED) return (long long)a.p.rows * a.p.H_kv * ((a.p.G + TILE_ROWS - 1) / TILE_ROWS) * ((((long long)a.budget << a.p.lg) + UNIT - 1) / UNIT);
+    return a.prefix[*a.tiles] * a.p.H_kv;
+}
+
+// The tile that holds unit x (the same in all lanes).
+template <bool LISTED>
+__device__ inline Tile find_tile(const AttendArgs& a, long long x) {
+    const PagedArgs& p = a.p;
+    Tile t;
+    if (LISTED) {
+        const int per_row = (p.G + TILE_ROWS - 1) / TILE_ROWS;
+        t.units = (int)((((long long)a.budget << p.lg) + UNIT - 1) / UNIT);
+        const long long i = x / t.units, per_head = (long long)p.rows * per_row;
+        t.at = i * t.units;
+        t.kvh = (int)(i / per_head);
+        t.row = (int)(i % per_head) / per_row;
+        t.j = (int)(i % per_head) % per_row;
+        t.b = paged_find(p, t.row);
+        t.any = t.b < p.B;
+        t.s = {0, 0, 0, 0};
+        if (t.any) {
+            t.s = paged_seq(p, t.b);
+            t.any = t.row >= t.s.row0 && t.row < t.s.row0 + t.s.n;
+        }
+        return t;
+    }
+    const int lane = threadIdx.x & 63, n = *a.tiles;
+    const long long per_head = a.prefix[n], y = x % per_head;
+    t.kvh = (int)(x / per_head);
+    int lo = 0, hi = n;                                    // prefix[lo] <= y < prefix[hi]
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const int k = __popcll(__builtin_amdgcn_ballot_w64(at < hi && a.prefix[min(at, hi - 1)] <= y)) - 1;
+        lo += k * step;
+        hi = min(hi, lo + step);
+    }
+    t.at = t.kvh * per_head + a.prefix[lo];
+    t.units = (int)(a.prefix[lo + 1] - a.prefix[lo]);
+    t.b = a.tile[lo].x;
+    t.j = a.tile[lo].y;
+    t.s = paged_seq(p, t.b);
+    t.row = 0;
+    t.any = true;
+    return t;
+}
+
+// The tile in scalar registers.
+__device__ inline Tile same_in_all(Tile t) {
+    auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    t.at = (long long)(((unsigned long long)(uint32_t)one((int)(t.at >> 32)) << 32) | (uint32_t)one((int)t.at));
+    t.units = one(t.units); t.kvh = one(t.kvh); t.b = one(t.b); t.j = one(t.j); t.row = one(t.row); t.any = one(t.any) != 0;
+    t.s = {one(t.s.row0), one(t.s.n), one(t.s.past), one(t.s.len)};
+    return t;
+}
+
+// Row r of a tile: its row of Q and head of the group; false where the tile has no such row.
+template <bool LISTED>
+__device__ inline bool tile_row(const AttendArgs& a, const Tile& t, int r, int& row, int& head, int& token) {
+    if (LISTED) {
+        head = t.j * TILE_ROWS + r;
+        row = t.row;
+        token = t.row - t.s.row0;
+        return head < a.p.G;
+    }
+    const int flat = t.j * TILE_ROWS + r;
+    token = flat / a.p.G;
+    head = flat - token * a.p.G;
+    row = t.s.row0 + token;
+    return token < t.s.n;
+}
+
+// ------------------------------------------------------------------------------------------------ products
+template <typename In, int DH> struct Rows {               // bf16
+    static constexpr int EPP = 8, KF = DH / 32, VF = DH / 16, NB = DH / 16;
+    static constexpr int PITCH = DH * 2 + 32;              // 16 rows read 32 bytes each without meeting on a bank
+    static constexpr int V_LDS = WAVE_KEYS * PITCH;
+};
+template <int DH> struct Rows<float, DH> {
+    static constexpr int EPP = 4, KF = DH / 16, VF = DH / 8, NB = DH / 16;
+    static constexpr int V_LDS = 0;
+};
+
+__device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <typename In, int DH> constexpr int rows_lds() {
+    constexpr int out = 4 * TILE_ROWS * (DH + 4) * 4, v = 4 * Rows<In, DH>::V_LDS;
+    return (out > v ? out : v) + 2 * 4 * TILE_ROWS * 4;
+}
+
+// A row of the output, or of a cut tile, from the thread that has DH / 16 columns of it.
+template <typename In, int DH>
+__device__ inline void store_out(In* to, const float (&o)[DH / 16], float f) {
+    if constexpr (sizeof(In) == 4) {
+#pragma unroll
+        for (int c = 0; c < DH / 16; c += 4) *reinterpret_cast<f32x4*>(to + c) = f32x4{o[c] * f, o[c + 1] * f, o[c + 2] * f, o[c + 3] * f};
+    } else {
+        uint32_t w[DH / 32];
+#pragma unroll
+        for (int c = 0; c < DH / 32; ++c) w[c] = bf16_pair(o[2 * c] * f, o[2 * c + 1] * f);
+        if constexpr (DH == 64) *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[1]};
+        else
+#pragma unroll
+            for (int c = 0; c < DH / 32; c += 4) *reinterpret_cast<u32x4*>(to + 2 * c) = u32x4{w[c], w[c + 1], w[c + 2], w[c + 3]};
+    }
+}
+
+template <typename In, int DH, bool LISTED>
+__global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_rows(AttendArgs a) {
+    using R = Rows<In, DH>;
+    constexpr int KF = R::KF, VF = R::VF, NB = R::NB;
+    extern __shared__ __align__(16) char lds[];
+    const PagedArgs& p = a.p;
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    float* obuf = reinterpret_cast<float*>(lds);           // [4][16][DH + 4], over the values' place
+    float* mbuf = reinterpret_cast<float*>(lds + rows_lds<In, DH>() - 2 * 4 * TILE_ROWS * 4);
+    float* lbuf = mbuf + 4 * TILE_ROWS;
+    const int me = by_xcd(blockIdx.x, gridDim.x);
+    const long long total = line_length<LISTED>(a), x0 = me * total / gridDim.x, x1 = (me + 1) * total / gridDim.x;
+
+    for (long long x = x0; x < x1;) {
+        const Tile t = same_in_all(find_tile<LISTED>(a, x));
+        const int k0 = (int)(x - t.at), k1 = (int)(min(x1, t.at + t.units) - t.at);
+        x = t.at + k1;
+        if (!t.any) continue;
+        // ---- queries: the operand of lane (column l16 = row of the tile)
+        int row, head, token;
+        const bool mine = tile_row<LISTED>(a, t, l16, row, head, token);
+        if (!mine) {                                       // (products with row 0, never stored)
+            int h0, t0;
+            tile_row<LISTED>(a, t, 0, row, h0, t0);
+            head = h0; token = t0;
+        }
+        const In* q = reinterpret_cast<const In*>(a.Q) + row * a.ldq + (long long)(t.kvh * p.G + head) * DH;
+        u32x4 qf[KF];
+#pragma unroll
+        for (int c = 0; c < KF; ++c) qf[c] = *reinterpret_cast<const u32x4*>(q + (c * 4 + g) * R::EPP);
+        const int limit = p.causal ? t.s.past + token + 1 : t.s.len;                  // keys below it are seen
+        const long long lrow = LISTED ? (long long)t.row * p.H_kv + t.kvh : 0;
+        const int32_t* list = LISTED ? a.list + lrow * a.budget : nullptr;
+        const int n_list = LISTED ? min(max(a.count[lrow], 0), a.budget) : 0;
+        const long long head_at = t.kvh * p.head_stride;
+
+        // 16 keys: their first position (NOWHERE: nothing to see) and place in the cache
+        auto resolve = [&](int v, int& pos, long long& at) {
+            pos = NOWHERE;
+            at = 0;
+            int lp = v >> p.lg, ps = v;
+            if (LISTED) {
+                if (lp >= n_list) return;
+                const int i = lp, before = i > 0 ? list[i - 1] : -1;
+                lp = list[i];
+                if (lp <= before || lp > (t.s.len - 1) >> p.lg) { raise(p, ADA_ERR_INDEX); return; }
+                ps = (lp << p.lg) + (v & ((1 << p.lg) - 1));
+            }
+            if (ps >= t.s.len) return;
+            const int page = p.table[t.b * p.table_stride + lp];
+            if (page < 0 || page >= p.pages) { raise(p, ADA_ERR_INDEX); return; }
+            pos = ps;
+            at = page * p.page_stride + (ps & ((1 << p.lg) - 1)) * p.slot_stride + head_at;
+        };
+        u32x4 kf[2][KF], vf[VF];
+        int pos[2];
+        long long at[2];
+        auto where = [&](int u) {                          // false: none of the wave's 32 keys of unit u is there
+            const int v = u * UNIT + wave * WAVE_KEYS;
+            resolve(v, pos[0], at[0]);
+            resolve(v + 16, pos[1], at[1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pos[i] = __builtin_amdgcn_readfirstlane(pos[i]);
+            return pos[0] != NOWHERE || pos[1] != NOWHERE;
+        };
+        // rows behind the sequence's end are not read: the last one stands in (its weight is 0)
+        auto row_of = [&](int i, int r, int& base) {
+            base = pos[i] != NOWHERE ? i : 1 - i;
+            return min(r, t.s.len - 1 - pos[base]);
+        };
+        auto fetch_k = [&]() {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                int base;
+                const int r = row_of(i, l16, base);
+                const In* k = reinterpret_cast<const In*>(p.K) + at[base] + r * p.slot_stride + g * R::EPP;
+#pragma unroll
+                for (int c = 0; c < KF; ++c) kf[i][c] = *reinterpret_cast<const u32x4*>(k + c * 4 * R::EPP);
+            }
+        };
+        auto fetch_v = [&]() {
+            if constexpr (sizeof(In) == 2) {               // rows by pieces, as LDS takes them
+                constexpr int PPR = DH / 8;
+#pragma unroll
+                for (int u = 0; u < VF; ++u) {
+                    const int i = u * 64 + lane, r32 = i / PPR;
+                    int b0, b1;
+                    const int r0 = row_of(0, r32 & 15, b0), r1 = row_of(1, r32 & 15, b1);
+                    const long long off = r32 < 16 ? at[b0] + r0 * p.slot_stride : at[b1] + r1 * p.slot_stride;
+                    vf[u] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const In*>(p.V) + off + (i % PPR) * 8);
+                }
+            } else {                                       // columns l16 DH / 16 .. of keys 4 g + e
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        int base;
+                        const int r = row_of(i, 4 * g + e, base);
+                        const In* v = reinterpret_cast<const In*>(p.V) + at[base] + r * p.slot_stride + l16 * (DH / 16);
+#pragma unroll
+                        for (int c = 0; c < DH / 64; ++c) vf[(i * 4 + e) * (DH / 64) + c] = *reinterpret_cast<const u32x4*>(v + 4 * c);
+                    }
+            }
+        };
+
+        float m_run = -INFINITY, l_run = 0.f;              // of query l16; the sum over this lane's keys only
+        f32x4 acc[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        bool have = where(k0);
+        if (have) { fetch_k(); fetch_v(); }
+        for (int u = k0; u < k1; ++u) {
+            if (!have) {
+                if (u + 1 < k1 && (have = where(u + 1))) { fetch_k(); fetch_v(); }
+                continue;
+            }
+            f32x4 s[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < KF; ++c) {
+                    if constexpr (sizeof(In) == 2) s[i] = mfma16(kf[i][c], qf[c], s[i]);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][c][e]), __uint_as_float(qf[c][e]), s[i], 0, 0, 0);
+                }
+            }
+            const int p0 = pos[0], p1 = pos[1];
+            char* vbuf = lds + wave * R::V_LDS;
+            if constexpr (sizeof(In) == 2) {
+                constexpr int PPR = DH / 8;
+#pragma unroll
+                for (int w = 0; w < VF; ++w) {
+                    const int i = w * 64 + lane;
+                    *reinterpret_cast<u32x4*>(vbuf + (i / PPR) * R::PITCH + (i % PPR) * 16) = vf[w];
+                }
+            }
+            have = u + 1 < k1 && where(u + 1);
+            if (have) {
+                fetch_k();
+                if constexpr (sizeof(In) == 2) fetch_v();
+            }
+            // weights in base 2 against a reference that moves only when it is passed by more than 10 (see ada_attn.hpp's kernels)
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[i][e] = (i ? p1 : p0) + 4 * g + e < limit ? s[i][e] * a.sc2 : -INFINITY;
+                    mx = fmaxf(mx, s[i][e]);
+                }
+            mx = max_over_groups(mx);
+            const bool grow = mx > m_run + 10.f;
+            if (__builtin_amdgcn_ballot_w64(grow) != 0ull) {
+                const float f = grow ? __builtin_amdgcn_exp2f(m_run - mx) : 1.f;
+                m_run = grow ? mx : m_run;
+                l_run *= f;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) acc[i] *= f;
+            }
+            const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[i][e] = __builtin_amdgcn_exp2f(s[i][e] - m_use);
+                    l_run += s[i][e];
+                }
+            if constexpr (sizeof(In) == 2) {
+                u32x4 hi, lo;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float w0 = s[w >> 1][2 * (w & 1)], w1 = s[w >> 1][2 * (w & 1) + 1];
+                    hi[w] = bf16_pair(w0, w1);
+                    lo[w] = bf16_pair(w0 - bf16_lo(hi[w]), w1 - bf16_hi(hi[w]));
+                }
+                // lane (g, l16) reads 4 columns of key 4 g + l16 / 4 and gets column l16 of keys 4 g .. 4 g + 3, as the weights lie
+                char* vr = vbuf + (4 * g + l16 / 4) * R::PITCH + (l16 % 4) * 8;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    typedef __attribute__((address_space(3))) s16x4* At;
+                    const u32x2 v0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(vr + i * 32)));
+                    const u32x2 v1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(vr + 16 * R::PITCH + i * 32)));
+                    const u32x4 v = {v0[0], v0[1], v1[0], v1[1]};
+                    acc[i] = mfma16(v, hi, acc[i]);
+                    acc[i] = mfma16(v, lo, acc[i]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int c = 0; c < NB; ++c)
+                            acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[(i * 4 + e) * (DH / 64) + c / 4][c % 4]), s[i][e], acc[c], 0, 0, 0);
+                if (have) fetch_v();
+            }
+        }
+        // ---- the four waves' sums, brought to the common maximum
+        l_run = sum_over_groups(l_run);
+        if (g == 0) { mbuf[wave * TILE_ROWS + l16] = m_run; lbuf[wave * TILE_ROWS + l16] = l_run; }
+        __syncthreads();                                   // (and nobody reads values from LDS any more)
+        float m_all = mbuf[l16];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) m_all = fmaxf(m_all, mbuf[w * TILE_ROWS + l16]);
+        const float f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_all);
+        float* ob = obuf + (wave * TILE_ROWS + l16) * (DH + 4);
+        if constexpr (sizeof(In) == 2) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) *reinterpret_cast<f32x4*>(ob + 16 * i + 4 * g) = acc[i] * f;
+        } else {                                           // row 4 g + e of block i is column (4 g + e) DH / 16 + i
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < NB; i += 4)
+                    *reinterpret_cast<f32x4*>(ob + (4 * g + e) * NB + i) = f32x4{acc[i][e], acc[i + 1][e], acc[i + 2][e], acc[i + 3][e]} * f;
+        }
+        __syncthreads();
+        {
+            const int r = tid >> 4, c0 = (tid & 15) * (DH / 16);
+            float o[DH / 16], m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m = fmaxf(m, mbuf[w * TILE_ROWS + r]);
+#pragma unroll
+            for (int c = 0; c < DH / 16; ++c) o[c] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float mw = mbuf[w * TILE_ROWS + r];
+                l += mw == -INFINITY ? 0.f : lbuf[w * TILE_ROWS + r] * __builtin_amdgcn_exp2f(mw - m);
+#pragma unroll
+                for (int c = 0; c < DH / 16; ++c) o[c] += obuf[(w * TILE_ROWS + r) * (DH + 4) + c0 + c];
+            }
+            if (k0 == 0 && k1 == t.units) {
+                int orow, ohead, otoken;
+                if (tile_row<LISTED>(a, t, r, orow, ohead, otoken))
+                    store_out<In, DH>(reinterpret_cast<In*>(a.out) + orow * a.ld_out + (long long)(t.kvh * p.G + ohead) * DH + c0, o, l > 0.f ? 1.f / l : 0.f);
+            } else {
+                const long long slot = 2LL * me + (k0 == 0 ? 1 : 0);
+                float* po = a.part_o + (slot * TILE_ROWS + r) * DH + c0;
+#pragma unroll
+                for (int c = 0; c < DH / 16; c += 4) *reinterpret_cast<f32x4*>(po + c) = f32x4{o[c], o[c + 1], o[c + 2], o[c + 3]};
+                if ((tid & 15) == 0) {
+                    a.part_ml[(slot * TILE_ROWS + r) * 2] = m;
+                    a.part_ml[(slot * TILE_ROWS + r) * 2 + 1] = l;
+                }
+            }
+        }
+        __syncthreads();                                   // the next tile's values take the same place
+    }
+}
+
+// Puts a cut tile together: the workgroup of the piece in which it begins does.
+template <typename In, int DH, bool LISTED>
+__global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
+    const int W = gridDim.x, me = blockIdx.x, tid = threadIdx.x;
+    const long long total = line_length<LISTED>(a), x0 = me * total / W, x1 = (me + 1) * total / W;
+    if (x0 >= x1 || x1 >= total) return;
+    const Tile t = find_tile<LISTED>(a, x1 - 1);
+    const long long end = t.at + t.units;
+    if (!t.any || end == x1 || t.at < x0) return;
+    int last = me;                                         // the pieces me .. last have a part of it
+    while ((last + 1) * total / W < end) ++last;
+    const int r = tid >> 4, c0 = (tid & 15) * (DH / 16);
+    int row, head, token;
+    if (!tile_row<LISTED>(a, t, r, row, head, token)) return;
+    float m = -INFINITY, l = 0.f, o[DH / 16];
+#pragma unroll
+    for (int c = 0; c < DH / 16; ++c) o[c] = 0.f;
+    for (int w = me; w <= last; ++w) {
+        if (w > me && w * total / W == (w + 1) * total / W) continue;                 // an empty piece
+        const long long slot = 2LL * w + (w == me ? 1 : 0);
+        const float mw = a.part_ml[(slot * TILE_ROWS + r) * 2], lw = a.part_ml[(slot * TILE_ROWS + r) * 2 + 1];
+        if (mw == -INFINITY) continue;
+        const float mn = fmaxf(m, mw), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), fw = __builtin_amdgcn_exp2f(mw - mn);
+        m = mn;
+        l = l * f + lw * fw;
+        const float* po = a.part_o + (slot * TILE_ROWS + r) * DH + c0;
+#pragma unroll
+        for (int c = 0; c < DH / 16; ++c) o[c] = o[c] * f + po[c] * fw;
+    }
+    store_out<In, DH>(reinterpret_cast<In*>(a.out) + row * a.ld_out + (long long)(t.kvh * a.p.G + head) * DH + c0, o, l > 0.f ? 1.f / l : 0.f);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+struct AttendWs { size_t prefix, tile, part_o, part_ml, bytes; };
+
+inline int attend_pieces() { return 4 * ada_hook_cus(); }
+
+inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
+    (void)dtype;
+    const size_t tiles = (size_t)((long long)p.rows * p.G / TILE_ROWS + p.B), parts = 2 * (size_t)attend_pieces();
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    AttendWs w;
+    w.prefix = 256;
+    w.tile = w.prefix + up((tiles + 1) * 8);
+    w.part_ml = w.tile + up(tiles * 8);
+    w.part_o = w.part_ml + up(parts * TILE_ROWS * 2 * 4);
+    w.bytes = w.part_o + up(parts * TILE_ROWS * (size_t)d_h * 4);
+    return w;
+}
+
+template <typename In, int DH, bool LISTED>
+hipError_t launch_rows(const AttendArgs& a, hipStream_t st) {
+    static std::once_flag once;
+    static hipError_t attr_err = hipSuccess;
+    std::call_once(once, [] {
+        attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_rows<In, DH, LISTED>), hipFuncAttributeMaxDynamicSharedMemorySize, rows_lds<In, DH>());
+    });
+    if (attr_err != hipSuccess) return attr_err;
+    const int W = attend_pieces();
+    {
+        ProfHook ps(ADA_K_ATTN, st);
+        hipLaunchKernelGGL((k_paged_rows<In, DH, LISTED>), dim3(W), dim3(256), (rows_lds<In, DH>()), st, a);
+    }
+    if (hipError_t e = hipGetLastError()) return e;
+    ProfHook ps(ADA_K_ATTN, st);
+    hipLaunchKernelGGL((k_paged_join<In, DH, LISTED>), dim3(W), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+template <typename In, int DH>
+hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
+    const AttendWs w = attend_ws(a.p, DH, sizeof(In) == 2 ? ADA_BF16 : ADA_F32);
+    char* at = reinterpret_cast<char*>(ws);
+    int* tiles = reinterpret_cast<int*>(at);
+    long long* prefix = reinterpret_cast<long long*>(at + w.prefix);
+    int2* tile = reinterpret_cast<int2*>(at + w.tile);
+    a.tiles = tiles; a.prefix = prefix; a.tile = tile;
+    a.part_o = reinterpret_cast<float*>(at + w.part_o);
+    a.part_ml = reinterpret_cast<float*>(at + w.part_ml);
+    if (a.list) return launch_rows<In, DH, true>(a, st);
+    {
+        ProfHook ps(ADA_K_ATTN, st);
+        hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, TILE_ROWS, UNIT, prefix, tile, tiles);
+    }
+    if (hipError_t e = hipGetLastError()) return e;
+    return launch_rows<In, DH, false>(a, st);
+}
