@@ -492,22 +492,41 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
     store_out<In, DH>(reinterpret_cast<In*>(a.out) + row * a.ld_out + (long long)(t.kvh * a.p.G + head) * DH + c0, o, l > 0.f ? 1.f / l : 0.f);
 }
 
+#include "ada_paged_tile.hpp"
+
 // ------------------------------------------------------------------------------------------------ host
 struct AttendWs { size_t prefix, tile, part_o, part_ml, bytes; };
 
-inline int attend_pieces() { return 4 * ada_hook_cus(); }
+// Chunks whose rows fill a good part of a 128-row tile go to ada_paged_tile.hpp's kernel.
+inline bool takes_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G >= 48; }
+
+inline int rows_pieces() { return 4 * ada_hook_cus(); }
+inline int tile_pieces(int d_h) { return (d_h > 128 ? 1 : 2) * ada_hook_cus(); }
 
 inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
-    (void)dtype;
-    const size_t tiles = (size_t)((long long)p.rows * p.G / TILE_ROWS + p.B), parts = 2 * (size_t)attend_pieces();
+    const size_t tiles = (size_t)((long long)p.rows * p.G / TILE_ROWS + p.B);
+    const size_t rows = (size_t)rows_pieces() * TILE_ROWS, tile_rows = takes_tiles(p, dtype) ? (size_t)tile_pieces(d_h) * 128 : 0;
+    const size_t parts = 2 * (rows > tile_rows ? rows : tile_rows);           // rows of cut tiles (listed pages always take 16-row ones)
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     AttendWs w;
     w.prefix = 256;
     w.tile = w.prefix + up((tiles + 1) * 8);
     w.part_ml = w.tile + up(tiles * 8);
-    w.part_o = w.part_ml + up(parts * TILE_ROWS * 2 * 4);
-    w.bytes = w.part_o + up(parts * TILE_ROWS * (size_t)d_h * 4);
+    w.part_o = w.part_ml + up(parts * 2 * 4);
+    w.bytes = w.part_o + up(parts * (size_t)d_h * 4);
     return w;
+}
+
+template <typename Kernel, typename Join>
+hipError_t launch_pieces(Kernel kernel, Join join, int W, int lds, const AttendArgs& a, hipStream_t st) {
+    {
+        ProfHook ps(ADA_K_ATTN, st);
+        hipLaunchKernelGGL(kernel, dim3(W), dim3(256), lds, st, a);
+    }
+    if (hipError_t e = hipGetLastError()) return e;
+    ProfHook ps(ADA_K_ATTN, st);
+    hipLaunchKernelGGL(join, dim3(W), dim3(256), 0, st, a);
+    return hipGetLastError();
 }
 
 template <typename In, int DH, bool LISTED>
@@ -518,20 +537,24 @@ hipError_t launch_rows(const AttendArgs& a, hipStream_t st) {
         attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_rows<In, DH, LISTED>), hipFuncAttributeMaxDynamicSharedMemorySize, rows_lds<In, DH>());
     });
     if (attr_err != hipSuccess) return attr_err;
-    const int W = attend_pieces();
-    {
-        ProfHook ps(ADA_K_ATTN, st);
-        hipLaunchKernelGGL((k_paged_rows<In, DH, LISTED>), dim3(W), dim3(256), (rows_lds<In, DH>()), st, a);
-    }
-    if (hipError_t e = hipGetLastError()) return e;
-    ProfHook ps(ADA_K_ATTN, st);
-    hipLaunchKernelGGL((k_paged_join<In, DH, LISTED>), dim3(W), dim3(256), 0, st, a);
-    return hipGetLastError();
+    return launch_pieces(&k_paged_rows<In, DH, LISTED>, &k_paged_join<In, DH, LISTED>, rows_pieces(), rows_lds<In, DH>(), a, st);
+}
+
+template <int DH>
+hipError_t launch_tiles(const AttendArgs& a, hipStream_t st) {
+    static std::once_flag once;
+    static hipError_t attr_err = hipSuccess;
+    std::call_once(once, [] {
+        attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_tile<DH>), hipFuncAttributeMaxDynamicSharedMemorySize, TileGeom<DH>::LDS);
+    });
+    if (attr_err != hipSuccess) return attr_err;
+    return launch_pieces(&k_paged_tile<DH>, &k_paged_tile_join<DH>, tile_pieces(DH), TileGeom<DH>::LDS, a, st);
 }
 
 template <typename In, int DH>
 hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
-    const AttendWs w = attend_ws(a.p, DH, sizeof(In) == 2 ? ADA_BF16 : ADA_F32);
+    constexpr int dtype = sizeof(In) == 2 ? ADA_BF16 : ADA_F32;
+    const AttendWs w = attend_ws(a.p, DH, dtype);
     char* at = reinterpret_cast<char*>(ws);
     int* tiles = reinterpret_cast<int*>(at);
     long long* prefix = reinterpret_cast<long long*>(at + w.prefix);
@@ -540,10 +563,13 @@ hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
     a.part_o = reinterpret_cast<float*>(at + w.part_o);
     a.part_ml = reinterpret_cast<float*>(at + w.part_ml);
     if (a.list) return launch_rows<In, DH, true>(a, st);
+    const bool chunks = takes_tiles(a.p, dtype);
     {
         ProfHook ps(ADA_K_ATTN, st);
-        hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, TILE_ROWS, UNIT, prefix, tile, tiles);
+        hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, chunks ? 128 : TILE_ROWS, chunks ? 64 : UNIT, prefix, tile, tiles);
     }
     if (hipError_t e = hipGetLastError()) return e;
+    if constexpr (dtype == ADA_BF16)
+        if (chunks) return launch_tiles<DH>(a, st);
     return launch_rows<In, DH, false>(a, st);
 }
