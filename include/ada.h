@@ -385,7 +385,7 @@ typedef struct {
     int dtype;
     int64_t page_stride;    /* elements; strides in whole 16-byte pieces, K, V and bounds 16-byte aligned */
     int64_t head_stride;
-    int64_t slot_stride;
+    int64_t slot_stride;    /* at most 2^25 */
 } ada_paged_cache;
 
 /*

@@ -21,6 +21,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int MAX_TOKENS = 1 << 26;                        // positions of a sequence
+constexpr long long MAX_SLOT_STRIDE = 1 << 25;             // 16 rows within 32-bit byte offsets
 constexpr int NOWHERE = 1 << 30;                           // a position that no row sees
 
 // What every kernel here is told about the cache and the new tokens.
@@ -108,6 +109,7 @@ int paged_args(const ada_paged_cache* c, const ada_paged_chunk* k, int H, int32_
     if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1)) != 0) return ADA_ERR_SHAPE;
     if (c->slot_stride < c->d_h || c->head_stride < c->d_h || c->page_stride < c->d_h) return ADA_ERR_SHAPE;
     if (c->slot_stride * esz % 16 || c->head_stride * esz % 16 || c->page_stride * esz % 16) return ADA_ERR_SHAPE;
+    if (c->slot_stride > MAX_SLOT_STRIDE) return ADA_ERR_SHAPE;
     if ((uintptr_t)c->K % 16 || (uintptr_t)c->V % 16 || (uintptr_t)c->bounds % 16) return ADA_ERR_SHAPE;
     if (k->B < 1 || k->B > ADA_MAX_BATCH || k->rows < 0 || k->rows > ADA_MAX_T || k->longest < 0 || k->longest > k->rows) return ADA_ERR_SHAPE;
     if (k->rows > 0 && k->longest < 1) return ADA_ERR_SHAPE;

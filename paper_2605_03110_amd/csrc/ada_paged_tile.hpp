@@ -52,10 +52,18 @@ __device__ inline void store_rows(const AttendArgs& a, const Tile& t, int row, i
             *reinterpret_cast<u32x2*>(to + 32 * i + 8 * w) = u32x2{bf16_pair(o[i][4 * w] * f, o[i][4 * w + 1] * f), bf16_pair(o[i][4 * w + 2] * f, o[i][4 * w + 3] * f)};
 }
 
+// 16 bytes per lane from `base` (the same in all lanes) + `off` bytes to `to` (the same) + 16 lane.  Written out because the compiler, which sees the
+// builtin write LDS, would wait for these loads in front of every transposed read of the other stage; a load without a destination register is waited for by the
+// loop's own barrier.
+__device__ inline void load_to_lds(const void* base, uint32_t off, char* to) {
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to;
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(at)), "v"(off), "s"(base) : "m0", "memory");
+}
+
 template <int DH>
 __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(AttendArgs a) {
     using G = TileGeom<DH>;
-    constexpr int KS = G::KS, NB = G::NB, PPR = G::PPR;
+    constexpr int KS = G::KS, NB = G::NB, PPR = G::PPR, PIECES = DH / 32;      // PIECES: 1 KB loads of a wave's 16 rows
     extern __shared__ __align__(16) char lds[];
     char* kbuf = lds;
     char* vbuf = lds + 2 * G::STAGE;
@@ -67,6 +75,13 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
     // where this lane's columns of a value row start in LDS for the transposed reads: rows 4 half + (lane & 15) / 4 + 8 n, columns 16 ((lane >> 4) & 1) + 4 (lane & 3)
     const int vrow = 4 * half + ((lane & 15) >> 2);
     const int vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    uint32_t koff[PIECES], voff[PIECES];                   // where this lane reads in 16 whole rows
+#pragma unroll
+    for (int c = 0; c < PIECES; ++c) {
+        const int r = c * (512 / DH) + lane / PPR;
+        koff[c] = (uint32_t)(r * p.slot_stride + G::key_slot(r, lane % PPR) * 8) * 2;
+        voff[c] = (uint32_t)(r * p.slot_stride + G::value_slot(r, lane % PPR) * 8) * 2;
+    }
 
     for (long long x = x0; x < x1;) {
         const Tile t = same_in_all(find_tile<false>(a, x));
@@ -87,76 +102,86 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
         const int all_see = __builtin_amdgcn_readfirstlane(limit);                    // by all rows of the wave (its first row is the earliest)
         const int last16 = (t.s.len - 1) & ~15;
         const int32_t* table = p.table + t.b * p.table_stride;
+        const long long head_at = t.kvh * p.head_stride;
         // lanes 0 .. 3: the pages of a unit's 16-key groups (behind the end: the last group again, whose keys nobody sees there)
         auto pages_of = [&](int u) { return table[min(u * G::KEYS + (lane & 3) * 16, last16) >> p.lg]; };
         auto bad_of = [&](int pg) { return (int)(__builtin_amdgcn_ballot_w64(pg < 0 || pg >= p.pages) & 15); };
-        auto issue = [&](int u, int stage, int pg) {       // the wave's 16 keys and values of unit u
+        // the wave's 16 rows of unit u's keys or values
+        auto issue = [&](const void* from, const uint32_t (&off)[PIECES], bool values, int u, int pg) {
             const int page = __builtin_amdgcn_readlane(pg, wave), pos = min(u * G::KEYS + wave * 16, last16);
             const bool ok = page >= 0 && page < p.pages;
-            // where there is no page a row of queries stands in: finite numbers, weight 0
-            const long long at = page * p.page_stride + (pos & ((1 << p.lg) - 1)) * p.slot_stride + t.kvh * p.head_stride;
-            const uint16_t* stand_in = reinterpret_cast<const uint16_t*>(a.Q) + t.s.row0 * a.ldq;
-            const uint16_t* ks = ok ? reinterpret_cast<const uint16_t*>(p.K) + at : stand_in;
-            const uint16_t* vs = ok ? reinterpret_cast<const uint16_t*>(p.V) + at : stand_in;
-            const long long stride = ok ? p.slot_stride : 0;
-            if (!ok && lane == 0) raise(p, ADA_ERR_INDEX);
+            char* to = (values ? vbuf : kbuf) + (u & 1) * G::STAGE + wave * 32 * DH;
+            const uint16_t* src = reinterpret_cast<const uint16_t*>(from) + page * p.page_stride + (pos & ((1 << p.lg) - 1)) * p.slot_stride + head_at;
+            if (ok && pos + 16 <= t.s.len) {
 #pragma unroll
-            for (int c = 0; c < DH / 32; ++c) {
-                const int r = c * (512 / DH) + lane / PPR, in = min(r, t.s.len - 1 - pos);
-                __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(ks + in * stride + G::key_slot(wave * 16 + r, lane % PPR) * 8),
-                                                 (void __attribute__((address_space(3)))*)(kbuf + stage * G::STAGE + wave * 32 * DH + c * 1024), 16, 0, 0);
+                for (int c = 0; c < PIECES; ++c) load_to_lds(src, off[c], to + c * 1024);
+                return;
+            }
+            // rows behind the end are not read: the last one stands in; where there is no page, a row of queries: finite numbers, weight 0
+            if (!ok) {
+                src = reinterpret_cast<const uint16_t*>(a.Q) + t.s.row0 * a.ldq;
+                if (lane == 0) raise(p, ADA_ERR_INDEX);
             }
 #pragma unroll
-            for (int c = 0; c < DH / 32; ++c) {
-                const int r = c * (512 / DH) + lane / PPR, in = min(r, t.s.len - 1 - pos);
-                __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(vs + in * stride + G::value_slot(wave * 16 + r, lane % PPR) * 8),
-                                                 (void __attribute__((address_space(3)))*)(vbuf + stage * G::STAGE + wave * 32 * DH + c * 1024), 16, 0, 0);
+            for (int c = 0; c < PIECES; ++c) {
+                const int r = c * (512 / DH) + lane / PPR, in = ok ? min(r, t.s.len - 1 - pos) : 0;
+                load_to_lds(src, (uint32_t)(in * p.slot_stride + (values ? G::value_slot(r, lane % PPR) : G::key_slot(r, lane % PPR)) * 8) * 2, to + c * 1024);
             }
         };
-        f32x16 acc_o[NB];
+        auto landed = [] {                                 // this wave's loads have landed and its reads have returned, and so have everybody's
+            __builtin_amdgcn_s_waitcnt(0x0070);
+            asm volatile("s_barrier" ::: "memory");
+        };
+        u32x4 kf[3][2];                                    // keys, read two steps ahead of their products
+        auto read_k = [&](const char* kc, int ks) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                kf[ks % 3][b] = *reinterpret_cast<const u32x4*>(kc + (b * 32 + l32) * DH * 2 + G::key_slot(l32, 2 * ks + half) * 16);
+        };
+        f32x16 acc_o[NB], s[2], s2[2];
 #pragma unroll
         for (int i = 0; i < NB; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
         float m_run = -INFINITY, l_run = 0.f;              // of query l32; the sum over this half's keys
-        int pg = pages_of(k0);
+        int pg0 = pages_of(k0), pg1 = pages_of(k0 + 1), pg2 = pages_of(k0 + 2);       // of units u, u + 1, u + 2
         __syncthreads();                                   // the tile before is done with LDS
-        issue(k0, 0, pg);
-        int bad = bad_of(pg);
-        pg = pages_of(k0 + 1);
-        for (int u = k0; u < k1; ++u) {
-            const int stage = (u - k0) & 1;
-            __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): this wave's part of the unit has landed
-            __builtin_amdgcn_s_barrier();
-            const int bad_now = bad;
-            if (u + 1 < k1) {
-                issue(u + 1, stage ^ 1, pg);
-                bad = bad_of(pg);
-                pg = pages_of(u + 2);
-            }
-            // ---- S^T: 64 keys x this wave's 32 queries
-            const char* kc = kbuf + stage * G::STAGE;
-            f32x16 s[2];
+        issue(p.K, koff, false, k0, pg0);
+        issue(p.V, voff, true, k0, pg0);
+        landed();
+        if (k0 + 1 < k1) issue(p.K, koff, false, k0 + 1, pg1);
+        {   // S^T of the first unit
+            const char* kc = kbuf + (k0 & 1) * G::STAGE;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+            read_k(kc, 0);
+            read_k(kc, 1);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + 2 < KS) read_k(kc, ks + 2);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const u32x4 kf = *reinterpret_cast<const u32x4*>(kc + (b * 32 + l32) * DH * 2 + G::key_slot(l32, 2 * ks + half) * 16);
-                    s[b] = mfma32(kf, qf[ks], s[b]);
-                }
+                for (int b = 0; b < 2; ++b) s[b] = mfma32(kf[ks % 3][b], qf[ks], s[b]);
+            }
+        }
+        for (int u = k0; u < k1; ++u) {
+            landed();                                      // keys of u + 1, values of u
+            if (u + 2 < k1) issue(p.K, koff, false, u + 2, pg2);
+            if (u + 1 < k1) issue(p.V, voff, true, u + 1, pg1);
+            const int bad = bad_of(pg0);
+            pg0 = pg1;
+            pg1 = pg2;
+            pg2 = pages_of(u + 3);
             // ---- weights in base 2 against a reference that moves when it is passed by more than 10
             const int key0 = u * G::KEYS;
-            if (key0 + G::KEYS > all_see || bad_now) {     // (the same for the wave)
+            if (key0 + G::KEYS > all_see || bad) {         // (the same for the wave)
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int k = b * 32 + (e & 3) + 8 * (e >> 2) + 4 * half;
-                        if (key0 + k >= limit || (bad_now >> (2 * b + (e >> 3))) & 1) s[b][e] = -INFINITY;
+                        if (key0 + k >= limit || (bad >> (2 * b + (e >> 3))) & 1) s[b][e] = -INFINITY;
                     }
             }
             float mx = -INFINITY;
@@ -176,17 +201,30 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
                     for (int e = 0; e < 16; ++e) acc_o[i][e] *= f;
             }
             const float m_use = m_run == -INFINITY ? 0.f : m_run;
-            u32x4 pf[4];                                   // weights, one bf16 number each (half a step: 2^-9), by 16 keys
+            // ---- S^T of the next unit beside the weights of this one (behind the last unit: of what lies in LDS, for nobody)
+            const char* kc = kbuf + ((u + 1) & 1) * G::STAGE;
+            u32x4 pf[4];                                   // weights, one bf16 number each, by 16 keys
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) {
+                for (int e = 0; e < 16; ++e) s2[b][e] = 0.f;
+            read_k(kc, 0);
+            read_k(kc, 1);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + 2 < KS) read_k(kc, ks + 2);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) s2[b] = mfma32(kf[ks % 3][b], qf[ks], s2[b]);
+#pragma unroll
+                for (int w = ks * 16 / KS; w < (ks + 1) * 16 / KS; ++w) {
+                    const int b = w >> 3, e = 2 * (w & 7);
                     const float w0 = __builtin_amdgcn_exp2f(s[b][e] * a.sc2 - m_use), w1 = __builtin_amdgcn_exp2f(s[b][e + 1] * a.sc2 - m_use);
                     l_run += w0 + w1;
                     pf[2 * b + (e >> 3)][(e & 7) >> 1] = bf16_pair(w0, w1);
                 }
+            }
             // ---- O^T += V^T P^T
-            const char* vc = vbuf + stage * G::STAGE + 8 * (lane & 1);
+            const char* vc = vbuf + (u & 1) * G::STAGE + 8 * (lane & 1);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -196,6 +234,8 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
                     const u32x2 v1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsAt)(vc + r1 * DH * 2 + G::value_slot(r1, 4 * i + vpiece) * 16)));
                     acc_o[i] = mfma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, pf[j], acc_o[i]);
                 }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) s[b] = s2[b];
         }
         const float l = sum_over_halves(l_run);
         if (k0 == 0 && k1 == t.units) {
