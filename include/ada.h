@@ -417,8 +417,10 @@ typedef struct {
  * Two sequences may share pages that are only read.  A page that a call appends to belongs to one sequence.
  */
 
-/* Bytes of workspace that ada_attention_paged and ada_attention_pages need for these sizes (256-byte aligned); it need not be
- * cleared.  0 for arguments that those calls refuse. */
+/* Bytes of workspace that ada_attention_paged and ada_attention_pages need for these sizes (256-byte aligned).  0 for arguments that those
+ * calls refuse.  The first ADA_PAGED_ZERO_BYTES of it must be zero before the first use (ada_workspace_init on them, or any memset); every
+ * call leaves them so.  Calls that share a workspace must not overlap in time; one that is abandoned part-way needs it cleared again. */
+#define ADA_PAGED_ZERO_BYTES 8192
 size_t ada_paged_workspace_bytes(const ada_paged_cache* cache, const ada_paged_chunk* chunk, int H);
 
 /*

@@ -28,6 +28,7 @@ FLAG_ATTN_CAUSAL = 8
 FLAG_GREEDY_COVER = 16
 FLAG_ROPE_PAIRS = 32
 SELECT_MAX_PAGES = 8192
+PAGED_ZERO_BYTES = 8192
 OK = 0
 
 SYMBOLS = ("ada_status_string", "ada_workspace_bytes", "ada_workspace_zero_bytes", "ada_workspace_init", "ada_select_full", "ada_cascade_step",
@@ -99,7 +100,7 @@ SCRATCH_BUDGET = {
     "k_attn_rep2ILi64E": 0,
     "k_attn_repIfL": 0,                        # and in fp32
     "k_paged_rowsI": 0,                        # the paged cache
-    "k_paged_joinI": 0,
+    "k_paged_tileI": 0,
     "k_cache_appendI": 0,
     "k_cache_boundsI": 0,
     "k_select_pagesI": 0,
@@ -763,11 +764,13 @@ def ada_paged_workspace_bytes(cache: PagedCache, chunk: Chunk, H: int) -> int:
 
 
 def paged_workspace(cache: PagedCache, chunk: Chunk, H: int) -> torch.Tensor:
-    """A workspace for ada_attention_paged and ada_attention_pages of these sizes (it holds nothing between calls)."""
+    """A workspace for ada_attention_paged and ada_attention_pages of these sizes, ready for use."""
     n = ada_paged_workspace_bytes(cache, chunk, H)
     if n == 0:
         raise ValueError("sizes that no paged attention takes")
-    return torch.empty(n, dtype=torch.uint8, device=cache.K.device)
+    ws = torch.empty(n, dtype=torch.uint8, device=cache.K.device)
+    ws[:PAGED_ZERO_BYTES].zero_()
+    return ws
 
 
 def _paged_rows(cache: PagedCache, chunk: Chunk, X: torch.Tensor, name: str, heads: Optional[int] = None) -> int:

@@ -1,9 +1,10 @@
 // Attention of new tokens over a paged cache, and over listed pages of it.
 //
 // A head of the cache and up to 16 of the query rows that read it (tokens x heads of the group, flat row = token * G + head) make a tile.  Its
-// keys come in units of 128; the units of all tiles stand in one line, which is cut into as many equal pieces as there are workgroups, so
-// that one long sequence and many short ones fill the chip alike.  A piece that holds a whole tile writes the output; a tile that is cut leaves
-// rows, maxima and sums per piece, which k_paged_join puts together in the order of the keys (the same result on every run).
+// keys come in units of 128; the tiles stand in one line, each as long as its units and what beginning it costs, and the line is cut into as many equal
+// pieces as there are workgroups, so that one long sequence and many short ones fill the chip alike.  A piece that holds a whole tile writes the
+// output; a tile that is cut leaves rows, maxima and sums per piece, and whoever of its pieces comes last puts them together in the order of
+// the keys (the same result on every run).
 //
 // Inside a unit each of the four waves takes 32 keys: S^T = K Q^T with keys straight from memory in registers (a lane's 16 bytes of one key are the operand
 // as it is), softmax over keys = registers and two lane swaps, O^T += V^T P^T with the weights as they come out of the first product.  In bf16 the values
@@ -20,16 +21,23 @@ struct AttendArgs {
     float sc2;                                             // log2(e) / sqrt(d_h)
     const int32_t *list, *count;                           // listed pages, or NULL
     int budget;
-    const long long* prefix;                               // [tiles + 1] units in front of a tile of one head (k_paged_plan)
+    const long long* prefix;                               // [tiles + 1] line in front of a tile of one head (k_paged_plan)
     const int2* tile;                                      // [tiles] its sequence and number in it
     const int* tiles;
-    float *part_o, *part_ml;                               // per piece two cut tiles: [16][DH] rows, [16][2] maxima and sums
+    int* arrived;                                          // [pieces] parts of the tile that begins in a piece and is cut; zero between calls
+    float *part_o, *part_ml;                               // per piece two cut tiles: rows, and [rows][2] maxima and sums
 };
 
 constexpr int TILE_ROWS = 16, UNIT = 128, WAVE_KEYS = 32;
+constexpr int BEGIN = 2;                                   // what beginning a tile costs, in units (its place, queries, first keys, outputs)
 
 // ------------------------------------------------------------------------------------------------ who does what
-// Units of every tile of one head, one workgroup.
+// How tiles stand in the line of one head of the cache.
+enum { CHUNKS,                                             // sequences of many tiles: as k_paged_plan has put down
+       TOKENS,                                             // a tile per sequence: every wave sums up the lengths itself
+       LISTED };                                           // listed pages: tiles of one row, all alike
+
+// One workgroup.
 __global__ __launch_bounds__(1024) void k_paged_plan(PagedArgs p, int tile_rows, int unit, long long* prefix, int2* tile, int* tiles) {
     __shared__ int base[ADA_MAX_BATCH + 1];
     __shared__ long long sums[16];
@@ -72,7 +80,7 @@ __global__ __launch_bounds__(1024) void k_paged_plan(PagedArgs p, int tile_rows,
             const int j = t - base[lo];
             const Seq s = paged_seq(p, lo);
             const int last = (int)min((long long)s.n - 1, ((long long)(j + 1) * tile_rows - 1) / p.G);
-            mine = ((p.causal ? s.past + last + 1 : s.len) + unit - 1) / unit;
+            mine = ((p.causal ? s.past + last + 1 : s.len) + unit - 1) / unit + BEGIN;
             tile[t] = {lo, j};
         }
         const long long upto = front + scan(mine);
@@ -86,83 +94,171 @@ __global__ __launch_bounds__(1024) void k_paged_plan(PagedArgs p, int tile_rows,
     if (tid == 0) { prefix[0] = 0; *tiles = n_tiles; }
 }
 
-// A tile of one head, and where its units stand in the line.
+// A tile of one head, and where it stands in the line.
 struct Tile {
-    long long at;                                          // its first unit
+    long long at;
     int units, kvh;
     Seq s;
-    int b, j;                                              // rows 16 j .. of the sequence's n G, or (listed) of the token's G
-    int row;                                               // listed: the token's row
-    bool any;                                              // somebody's (listed: the row may be nobody's)
+    int b, j;                                              // rows j * (rows of a tile) .. of the sequence's n G, or (LISTED) of the token's G
+    int row;                                               // LISTED: the token's row
+    bool any;                                              // somebody's (LISTED: the row may be nobody's)
 };
 
-template <bool LISTED>
-__device__ inline long long line_length(const AttendArgs& a) {
-    if (LISTED) return (long long)a.p.rows * a.p.H_kv * ((a.p.G + TILE_ROWS - 1) / TILE_ROWS) * ((((long long)a.budget << a.p.lg) + UNIT - 1) / UNIT);
-    return a.prefix[*a.tiles] * a.p.H_kv;
-}
-
-// The tile that holds unit x (the same in all lanes).
-template <bool LISTED>
-__device__ inline Tile find_tile(const AttendArgs& a, long long x) {
-    const PagedArgs& p = a.p;
-    Tile t;
-    if (LISTED) {
-        const int per_row = (p.G + TILE_ROWS - 1) / TILE_ROWS;
-        t.units = (int)((((long long)a.budget << p.lg) + UNIT - 1) / UNIT);
-        const long long i = x / t.units, per_head = (long long)p.rows * per_row;
-        t.at = i * t.units;
-        t.kvh = (int)(i / per_head);
-        t.row = (int)(i % per_head) / per_row;
-        t.j = (int)(i % per_head) % per_row;
-        t.b = paged_find(p, t.row);
-        t.any = t.b < p.B;
-        t.s = {0, 0, 0, 0};
-        if (t.any) {
-            t.s = paged_seq(p, t.b);
-            t.any = t.row >= t.s.row0 && t.row < t.s.row0 + t.s.n;
+template <int MODE> struct Line {
+    const AttendArgs& a;
+    long long per_head, total;
+    int units;                                             // LISTED: of every tile
+    long long upto;                                        // TOKENS: the line up to and with sequence `lane` of the first 64
+    __device__ explicit Line(const AttendArgs& args) : a(args), units(0), upto(0) {
+        const PagedArgs& p = a.p;
+        if (MODE == LISTED) {
+            units = (int)((((long long)a.budget << p.lg) + UNIT - 1) / UNIT);
+            per_head = (long long)p.rows * ((p.G + TILE_ROWS - 1) / TILE_ROWS) * (units + BEGIN);
+        } else if (MODE == TOKENS) {
+            upto = sums(0);
+            per_head = scalar(__shfl(upto, 63, 64));
+            for (int b0 = 64; b0 < p.B; b0 += 64) per_head += scalar(__shfl(sums(b0), 63, 64));
+        } else {
+            per_head = a.prefix[*a.tiles];
         }
+        per_head = scalar(per_head);
+        total = per_head * p.H_kv;
+    }
+    __device__ static int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+    __device__ static long long scalar(long long v) {
+        return (long long)(((unsigned long long)(uint32_t)scalar((int)(v >> 32)) << 32) | (uint32_t)scalar((int)v));
+    }
+    // inclusive sums of the lengths of sequences b0 .. b0 + 63
+    __device__ long long sums(int b0) const {
+        const int lane = threadIdx.x & 63;
+        long long v = 0;
+        if (b0 + lane < a.p.B) {
+            const Seq s = paged_seq(a.p, b0 + lane);
+            if (s.n > 0) v = (s.len + UNIT - 1) / UNIT + BEGIN;
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const long long u = __shfl_up(v, o, 64);
+            if (lane >= o) v += u;
+        }
+        return v;
+    }
+    // The tile at x, all of it in scalar registers.
+    __device__ Tile find(long long x) const {
+        const PagedArgs& p = a.p;
+        const int lane = threadIdx.x & 63;
+        Tile t;
+        t.s = {0, 0, 0, 0};
+        t.row = 0;
+        t.j = 0;
+        t.any = true;
+        t.kvh = scalar((int)(x / per_head));
+        const long long y = x - t.kvh * per_head;
+        if (MODE == LISTED) {
+            const int per_row = (p.G + TILE_ROWS - 1) / TILE_ROWS;
+            const long long i = y / (units + BEGIN);
+            t.units = units;
+            t.at = scalar(t.kvh * per_head + i * (units + BEGIN));
+            t.row = scalar((int)(i / per_row));
+            t.j = scalar((int)(i % per_row));
+            t.b = scalar(paged_find(p, t.row));
+            t.any = t.b < p.B;
+            if (!t.any) return t;
+        } else if (MODE == TOKENS) {
+            long long front = 0, v = upto;
+            int b0 = 0;
+            for (;;) {
+                const long long all = __shfl(v, 63, 64);
+                if (y < front + all || b0 + 64 >= p.B) break;
+                front += all;
+                b0 += 64;
+                v = sums(b0);
+            }
+            const int in = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(front + v > y)) - 1;
+            t.b = scalar(b0 + in);
+            t.at = scalar(t.kvh * per_head + front + (in > 0 ? __shfl(v, in - 1, 64) : 0));
+        } else {
+            int lo = 0, hi = *a.tiles;                     // prefix[lo] <= y < prefix[hi]
+            while (hi - lo > 1) {
+                const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+                const int k = __popcll(__builtin_amdgcn_ballot_w64(at < hi && a.prefix[min(at, hi - 1)] <= y)) - 1;
+                lo += k * step;
+                hi = min(hi, lo + step);
+            }
+            lo = scalar(lo);
+            t.at = scalar(t.kvh * per_head + a.prefix[lo]);
+            t.units = scalar((int)(a.prefix[lo + 1] - a.prefix[lo])) - BEGIN;
+            t.b = scalar(a.tile[lo].x);
+            t.j = scalar(a.tile[lo].y);
+        }
+        const Seq s = paged_seq(p, t.b);
+        t.s = {scalar(s.row0), scalar(s.n), scalar(s.past), scalar(s.len)};
+        if (MODE == TOKENS) t.units = (t.s.len + UNIT - 1) / UNIT;
+        if (MODE == LISTED) t.any = t.row >= t.s.row0 && t.row < t.s.row0 + t.s.n;
         return t;
     }
-    const int lane = threadIdx.x & 63, n = *a.tiles;
-    const long long per_head = a.prefix[n], y = x % per_head;
-    t.kvh = (int)(x / per_head);
-    int lo = 0, hi = n;                                    // prefix[lo] <= y < prefix[hi]
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
-        const int k = __popcll(__builtin_amdgcn_ballot_w64(at < hi && a.prefix[min(at, hi - 1)] <= y)) - 1;
-        lo += k * step;
-        hi = min(hi, lo + step);
+};
+
+// The workgroup's piece of the line: x0 .. x1 - 1 of `pieces`.
+struct Piece {
+    long long total, x0, x1;
+    int me, pieces;
+    __device__ explicit Piece(long long length) : total(length) {
+        pieces = (int)min((long long)gridDim.x, total);    // (none is empty)
+        me = pieces == (int)gridDim.x ? by_xcd(blockIdx.x, pieces) : (int)blockIdx.x;
+        x0 = me < pieces ? from(me) : 0;
+        x1 = me < pieces ? from(me + 1) : 0;
     }
-    t.at = t.kvh * per_head + a.prefix[lo];
-    t.units = (int)(a.prefix[lo + 1] - a.prefix[lo]);
-    t.b = a.tile[lo].x;
-    t.j = a.tile[lo].y;
-    t.s = paged_seq(p, t.b);
-    t.row = 0;
-    t.any = true;
-    return t;
+    __device__ long long from(int w) const { return w * total / pieces; }
+    __device__ int of(long long x) const { return (int)(((x + 1) * pieces - 1) / total); }
+};
+
+// A tile's units in a piece: k0 .. k1 - 1.
+struct Part {
+    int k0, k1;
+    __device__ Part(const Piece& c, const Tile& t, long long x) {
+        k0 = (int)max(x - t.at - BEGIN, 0LL);
+        k1 = (int)min(max(c.x1 - t.at - BEGIN, 0LL), (long long)t.units);
+    }
+    __device__ bool whole(const Tile& t) const { return k0 == 0 && k1 == t.units; }
+    __device__ long long slot(const Piece& c) const { return 2LL * c.me + (k0 == 0 ? 1 : 0); }
+};
+
+// Parts of cut tiles pass between XCDs, each of which has an L2 of its own: stored through it, read past it.  (Fences instead, which write back and drop
+// whole L2s: 64 single tokens at 100 to 8191 keys took 382 us.)
+__device__ inline void put(float* at, float x, float y) {
+    const f32x2 v = {x, y};
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(at), __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline f32x2 get(const float* at) {
+    return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
-// The tile in scalar registers.
-__device__ inline Tile same_in_all(Tile t) {
-    auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    t.at = (long long)(((unsigned long long)(uint32_t)one((int)(t.at >> 32)) << 32) | (uint32_t)one((int)t.at));
-    t.units = one(t.units); t.kvh = one(t.kvh); t.b = one(t.b); t.j = one(t.j); t.row = one(t.row); t.any = one(t.any) != 0;
-    t.s = {one(t.s.row0), one(t.s.n), one(t.s.past), one(t.s.len)};
-    return t;
+// Behind the stores of a cut tile's part: true in the workgroup that comes last, with the pieces first .. last that have one.  flag: a word in LDS.
+__device__ inline bool comes_last(const AttendArgs& a, const Piece& c, const Tile& t, int& first, int& last, int* flag) {
+    first = c.of(t.at + BEGIN);
+    last = c.of(t.at + BEGIN + t.units - 1);
+    __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): this wave's stores have arrived
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const bool all = __hip_atomic_fetch_add(a.arrived + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == last - first;
+        if (all) __hip_atomic_store(a.arrived + first, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // as it was found
+        *flag = all;
+    }
+    __syncthreads();
+    return *flag != 0;
 }
 
-// Row r of a tile: its row of Q and head of the group; false where the tile has no such row.
-template <bool LISTED>
+// Row r of a tile of ROWS: its row of Q and head of the group; false where the tile has no such row.
+template <int MODE, int ROWS>
 __device__ inline bool tile_row(const AttendArgs& a, const Tile& t, int r, int& row, int& head, int& token) {
-    if (LISTED) {
-        head = t.j * TILE_ROWS + r;
+    if (MODE == LISTED) {
+        head = t.j * ROWS + r;
         row = t.row;
         token = t.row - t.s.row0;
         return head < a.p.G;
     }
-    const int flat = t.j * TILE_ROWS + r;
+    const int flat = t.j * ROWS + r;
     token = flat / a.p.G;
     head = flat - token * a.p.G;
     row = t.s.row0 + token;
@@ -186,7 +282,7 @@ __device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
 
 template <typename In, int DH> constexpr int rows_lds() {
     constexpr int out = 4 * TILE_ROWS * (DH + 4) * 4, v = 4 * Rows<In, DH>::V_LDS;
-    return (out > v ? out : v) + 2 * 4 * TILE_ROWS * 4;
+    return (out > v ? out : v) + 2 * 4 * TILE_ROWS * 4 + 16;
 }
 
 // A row of the output, or of a cut tile, from the thread that has DH / 16 columns of it.
@@ -206,7 +302,7 @@ __device__ inline void store_out(In* to, const float (&o)[DH / 16], float f) {
     }
 }
 
-template <typename In, int DH, bool LISTED>
+template <typename In, int DH, int MODE>
 __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_rows(AttendArgs a) {
     using R = Rows<In, DH>;
     constexpr int KF = R::KF, VF = R::VF, NB = R::NB;
@@ -215,22 +311,25 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     float* obuf = reinterpret_cast<float*>(lds);           // [4][16][DH + 4], over the values' place
-    float* mbuf = reinterpret_cast<float*>(lds + rows_lds<In, DH>() - 2 * 4 * TILE_ROWS * 4);
+    float* mbuf = reinterpret_cast<float*>(lds + rows_lds<In, DH>() - 2 * 4 * TILE_ROWS * 4 - 16);
     float* lbuf = mbuf + 4 * TILE_ROWS;
-    const int me = by_xcd(blockIdx.x, gridDim.x);
-    const long long total = line_length<LISTED>(a), x0 = me * total / gridDim.x, x1 = (me + 1) * total / gridDim.x;
+    int* flag = reinterpret_cast<int*>(lbuf + 4 * TILE_ROWS);
+    const Line<MODE> line(a);
+    if (line.total == 0) return;
+    const Piece piece(line.total);
 
-    for (long long x = x0; x < x1;) {
-        const Tile t = same_in_all(find_tile<LISTED>(a, x));
-        const int k0 = (int)(x - t.at), k1 = (int)(min(x1, t.at + t.units) - t.at);
-        x = t.at + k1;
-        if (!t.any) continue;
+    for (long long x = piece.x0; x < piece.x1;) {
+        const Tile t = line.find(x);
+        const Part part(piece, t, x);
+        const int k0 = part.k0, k1 = part.k1;
+        x = t.at + BEGIN + t.units;
+        if (!t.any || k0 >= k1) continue;
         // ---- queries: the operand of lane (column l16 = row of the tile)
         int row, head, token;
-        const bool mine = tile_row<LISTED>(a, t, l16, row, head, token);
+        const bool mine = tile_row<MODE, TILE_ROWS>(a, t, l16, row, head, token);
         if (!mine) {                                       // (products with row 0, never stored)
             int h0, t0;
-            tile_row<LISTED>(a, t, 0, row, h0, t0);
+            tile_row<MODE, TILE_ROWS>(a, t, 0, row, h0, t0);
             head = h0; token = t0;
         }
         const In* q = reinterpret_cast<const In*>(a.Q) + row * a.ldq + (long long)(t.kvh * p.G + head) * DH;
@@ -238,9 +337,9 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
 #pragma unroll
         for (int c = 0; c < KF; ++c) qf[c] = *reinterpret_cast<const u32x4*>(q + (c * 4 + g) * R::EPP);
         const int limit = p.causal ? t.s.past + token + 1 : t.s.len;                  // keys below it are seen
-        const long long lrow = LISTED ? (long long)t.row * p.H_kv + t.kvh : 0;
-        const int32_t* list = LISTED ? a.list + lrow * a.budget : nullptr;
-        const int n_list = LISTED ? min(max(a.count[lrow], 0), a.budget) : 0;
+        const long long lrow = MODE == LISTED ? (long long)t.row * p.H_kv + t.kvh : 0;
+        const int32_t* list = MODE == LISTED ? a.list + lrow * a.budget : nullptr;
+        const int n_list = MODE == LISTED ? min(max(a.count[lrow], 0), a.budget) : 0;
         const long long head_at = t.kvh * p.head_stride;
 
         // 16 keys: their first position (NOWHERE: nothing to see) and place in the cache
@@ -248,7 +347,7 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
             pos = NOWHERE;
             at = 0;
             int lp = v >> p.lg, ps = v;
-            if (LISTED) {
+            if (MODE == LISTED) {
                 if (lp >= n_list) return;
                 const int i = lp, before = i > 0 ? list[i - 1] : -1;
                 lp = list[i];
@@ -441,18 +540,37 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
 #pragma unroll
                 for (int c = 0; c < DH / 16; ++c) o[c] += obuf[(w * TILE_ROWS + r) * (DH + 4) + c0 + c];
             }
-            if (k0 == 0 && k1 == t.units) {
-                int orow, ohead, otoken;
-                if (tile_row<LISTED>(a, t, r, orow, ohead, otoken))
-                    store_out<In, DH>(reinterpret_cast<In*>(a.out) + orow * a.ld_out + (long long)(t.kvh * p.G + ohead) * DH + c0, o, l > 0.f ? 1.f / l : 0.f);
+            int orow, ohead, otoken;
+            const bool stored = tile_row<MODE, TILE_ROWS>(a, t, r, orow, ohead, otoken);
+            In* to = reinterpret_cast<In*>(a.out) + orow * a.ld_out + (long long)(t.kvh * p.G + ohead) * DH + c0;
+            if (part.whole(t)) {
+                if (stored) store_out<In, DH>(to, o, l > 0.f ? 1.f / l : 0.f);
             } else {
-                const long long slot = 2LL * me + (k0 == 0 ? 1 : 0);
+                const long long slot = part.slot(piece);
                 float* po = a.part_o + (slot * TILE_ROWS + r) * DH + c0;
 #pragma unroll
-                for (int c = 0; c < DH / 16; c += 4) *reinterpret_cast<f32x4*>(po + c) = f32x4{o[c], o[c + 1], o[c + 2], o[c + 3]};
-                if ((tid & 15) == 0) {
-                    a.part_ml[(slot * TILE_ROWS + r) * 2] = m;
-                    a.part_ml[(slot * TILE_ROWS + r) * 2 + 1] = l;
+                for (int c = 0; c < DH / 16; c += 2) put(po + c, o[c], o[c + 1]);
+                if ((tid & 15) == 0) put(a.part_ml + (slot * TILE_ROWS + r) * 2, m, l);
+                int first, last;
+                if (comes_last(a, piece, t, first, last, flag) && stored) {
+                    m = -INFINITY;
+                    l = 0.f;
+#pragma unroll
+                    for (int c = 0; c < DH / 16; ++c) o[c] = 0.f;
+#pragma unroll 4
+                    for (int w = first; w <= last; ++w) {
+                        const long long s2 = (2LL * w + (w == first ? 1 : 0)) * TILE_ROWS + r;
+                        const f32x2 ml = get(a.part_ml + s2 * 2);
+                        f32x2 v[DH / 32];
+#pragma unroll
+                        for (int c = 0; c < DH / 32; ++c) v[c] = get(a.part_o + s2 * DH + c0 + 2 * c);
+                        const float mn = fmaxf(m, ml[0]), f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), f1 = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - mn);
+                        m = mn;
+                        l = l * f0 + ml[1] * f1;
+#pragma unroll
+                        for (int c = 0; c < DH / 16; ++c) o[c] = o[c] * f0 + v[c / 2][c % 2] * f1;
+                    }
+                    store_out<In, DH>(to, o, l > 0.f ? 1.f / l : 0.f);
                 }
             }
         }
@@ -460,47 +578,15 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
     }
 }
 
-// Puts a cut tile together: the workgroup of the piece in which it begins does.
-template <typename In, int DH, bool LISTED>
-__global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
-    const int W = gridDim.x, me = blockIdx.x, tid = threadIdx.x;
-    const long long total = line_length<LISTED>(a), x0 = me * total / W, x1 = (me + 1) * total / W;
-    if (x0 >= x1 || x1 >= total) return;
-    const Tile t = find_tile<LISTED>(a, x1 - 1);
-    const long long end = t.at + t.units;
-    if (!t.any || end == x1 || t.at < x0) return;
-    int last = me;                                         // the pieces me .. last have a part of it
-    while ((last + 1) * total / W < end) ++last;
-    const int r = tid >> 4, c0 = (tid & 15) * (DH / 16);
-    int row, head, token;
-    if (!tile_row<LISTED>(a, t, r, row, head, token)) return;
-    float m = -INFINITY, l = 0.f, o[DH / 16];
-#pragma unroll
-    for (int c = 0; c < DH / 16; ++c) o[c] = 0.f;
-    for (int w = me; w <= last; ++w) {
-        if (w > me && w * total / W == (w + 1) * total / W) continue;                 // an empty piece
-        const long long slot = 2LL * w + (w == me ? 1 : 0);
-        const float mw = a.part_ml[(slot * TILE_ROWS + r) * 2], lw = a.part_ml[(slot * TILE_ROWS + r) * 2 + 1];
-        if (mw == -INFINITY) continue;
-        const float mn = fmaxf(m, mw), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), fw = __builtin_amdgcn_exp2f(mw - mn);
-        m = mn;
-        l = l * f + lw * fw;
-        const float* po = a.part_o + (slot * TILE_ROWS + r) * DH + c0;
-#pragma unroll
-        for (int c = 0; c < DH / 16; ++c) o[c] = o[c] * f + po[c] * fw;
-    }
-    store_out<In, DH>(reinterpret_cast<In*>(a.out) + row * a.ld_out + (long long)(t.kvh * a.p.G + head) * DH + c0, o, l > 0.f ? 1.f / l : 0.f);
-}
-
 #include "ada_paged_tile.hpp"
 
 // ------------------------------------------------------------------------------------------------ host
-struct AttendWs { size_t prefix, tile, part_o, part_ml, bytes; };
+struct AttendWs { size_t tiles, prefix, tile, part_o, part_ml, bytes; };
 
 // Chunks whose rows fill a good part of a 128-row tile go to ada_paged_tile.hpp's kernel.
 inline bool takes_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G >= 48; }
 
-inline int rows_pieces() { return 4 * ada_hook_cus(); }
+inline int rows_pieces() { return 4 * ada_hook_cus() < ADA_PAGED_ZERO_BYTES / 4 ? 4 * ada_hook_cus() : ADA_PAGED_ZERO_BYTES / 4; }
 inline int tile_pieces(int d_h) { return (d_h > 128 ? 1 : 2) * ada_hook_cus(); }
 
 inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
@@ -509,7 +595,8 @@ inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
     const size_t parts = 2 * (rows > tile_rows ? rows : tile_rows);           // rows of cut tiles (listed pages always take 16-row ones)
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     AttendWs w;
-    w.prefix = 256;
+    w.tiles = ADA_PAGED_ZERO_BYTES;                        // behind what is zero between calls
+    w.prefix = w.tiles + 256;
     w.tile = w.prefix + up((tiles + 1) * 8);
     w.part_ml = w.tile + up(tiles * 8);
     w.part_o = w.part_ml + up(parts * 2 * 4);
@@ -517,38 +604,28 @@ inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
     return w;
 }
 
-template <typename Kernel, typename Join>
-hipError_t launch_pieces(Kernel kernel, Join join, int W, int lds, const AttendArgs& a, hipStream_t st) {
-    {
-        ProfHook ps(ADA_K_ATTN, st);
-        hipLaunchKernelGGL(kernel, dim3(W), dim3(256), lds, st, a);
-    }
-    if (hipError_t e = hipGetLastError()) return e;
+// A kernel that needs more LDS than a launch gets unasked.
+template <typename Kernel>
+hipError_t launch_pieces(Kernel kernel, std::once_flag& once, hipError_t& attr_err, int pieces, int lds, const AttendArgs& a, hipStream_t st) {
+    std::call_once(once, [&] { attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds); });
+    if (attr_err != hipSuccess) return attr_err;
     ProfHook ps(ADA_K_ATTN, st);
-    hipLaunchKernelGGL(join, dim3(W), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kernel, dim3(pieces), dim3(256), lds, st, a);
     return hipGetLastError();
 }
 
-template <typename In, int DH, bool LISTED>
+template <typename In, int DH, int MODE>
 hipError_t launch_rows(const AttendArgs& a, hipStream_t st) {
     static std::once_flag once;
     static hipError_t attr_err = hipSuccess;
-    std::call_once(once, [] {
-        attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_rows<In, DH, LISTED>), hipFuncAttributeMaxDynamicSharedMemorySize, rows_lds<In, DH>());
-    });
-    if (attr_err != hipSuccess) return attr_err;
-    return launch_pieces(&k_paged_rows<In, DH, LISTED>, &k_paged_join<In, DH, LISTED>, rows_pieces(), rows_lds<In, DH>(), a, st);
+    return launch_pieces(&k_paged_rows<In, DH, MODE>, once, attr_err, rows_pieces(), rows_lds<In, DH>(), a, st);
 }
 
 template <int DH>
 hipError_t launch_tiles(const AttendArgs& a, hipStream_t st) {
     static std::once_flag once;
     static hipError_t attr_err = hipSuccess;
-    std::call_once(once, [] {
-        attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_tile<DH>), hipFuncAttributeMaxDynamicSharedMemorySize, TileGeom<DH>::LDS);
-    });
-    if (attr_err != hipSuccess) return attr_err;
-    return launch_pieces(&k_paged_tile<DH>, &k_paged_tile_join<DH>, tile_pieces(DH), TileGeom<DH>::LDS, a, st);
+    return launch_pieces(&k_paged_tile<DH>, once, attr_err, tile_pieces(DH), TileGeom<DH>::LDS, a, st);
 }
 
 template <typename In, int DH>
@@ -556,14 +633,16 @@ hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
     constexpr int dtype = sizeof(In) == 2 ? ADA_BF16 : ADA_F32;
     const AttendWs w = attend_ws(a.p, DH, dtype);
     char* at = reinterpret_cast<char*>(ws);
-    int* tiles = reinterpret_cast<int*>(at);
+    int* tiles = reinterpret_cast<int*>(at + w.tiles);
     long long* prefix = reinterpret_cast<long long*>(at + w.prefix);
     int2* tile = reinterpret_cast<int2*>(at + w.tile);
+    a.arrived = reinterpret_cast<int*>(at);
     a.tiles = tiles; a.prefix = prefix; a.tile = tile;
     a.part_o = reinterpret_cast<float*>(at + w.part_o);
     a.part_ml = reinterpret_cast<float*>(at + w.part_ml);
-    if (a.list) return launch_rows<In, DH, true>(a, st);
+    if (a.list) return launch_rows<In, DH, LISTED>(a, st);
     const bool chunks = takes_tiles(a.p, dtype);
+    if (!chunks && (long long)a.p.longest * a.p.G <= TILE_ROWS) return launch_rows<In, DH, TOKENS>(a, st);
     {
         ProfHook ps(ADA_K_ATTN, st);
         hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, chunks ? 128 : TILE_ROWS, chunks ? 64 : UNIT, prefix, tile, tiles);
@@ -571,5 +650,5 @@ hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
     if (hipError_t e = hipGetLastError()) return e;
     if constexpr (dtype == ADA_BF16)
         if (chunks) return launch_tiles<DH>(a, st);
-    return launch_rows<In, DH, false>(a, st);
+    return launch_rows<In, DH, CHUNKS>(a, st);
 }

@@ -13,7 +13,7 @@ typedef __attribute__((address_space(3))) s16x4* LdsAt;
 
 template <int DH> struct TileGeom {
     static constexpr int WAVES = 4, ROWS = 32 * WAVES, KEYS = 64, KS = DH / 16, NB = DH / 32, PPR = DH / 8;
-    static constexpr int STAGE = KEYS * DH * 2, LDS = 4 * STAGE;               // keys and values, twice
+    static constexpr int STAGE = KEYS * DH * 2, LDS = 4 * STAGE + 16;          // keys and values, twice; comes_last's word
     static constexpr int PER_CU = DH > 128 ? 1 : 2;
     __device__ static int key_slot(int row, int piece) { return piece ^ (row & (PPR >= 16 ? 15 : 7)); }
     __device__ static int value_slot(int row, int piece) { return piece ^ (PPR >= 16 ? (row & 3) << 2 : ((row >> 1) & 1) << 2); }
@@ -29,16 +29,6 @@ __device__ inline float max_over_halves(float v) {
 __device__ inline float sum_over_halves(float v) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-// Row r of a tile: see tile_row.
-template <int ROWS>
-__device__ inline bool chunk_row(const AttendArgs& a, const Tile& t, int r, int& row, int& head, int& token) {
-    const int flat = t.j * ROWS + r;
-    token = flat / a.p.G;
-    head = flat - token * a.p.G;
-    row = t.s.row0 + token;
-    return token < t.s.n;
 }
 
 // A wave's 32 rows to the output: lane has columns 32 i + 8 w + 4 half .. of row l32.
@@ -70,8 +60,9 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
     const PagedArgs& p = a.p;
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int me = by_xcd(blockIdx.x, gridDim.x);
-    const long long total = line_length<false>(a), x0 = me * total / gridDim.x, x1 = (me + 1) * total / gridDim.x;
+    const Line<CHUNKS> line(a);
+    if (line.total == 0) return;
+    const Piece piece(line.total);
     // where this lane's columns of a value row start in LDS for the transposed reads: rows 4 half + (lane & 15) / 4 + 8 n, columns 16 ((lane >> 4) & 1) + 4 (lane & 3)
     const int vrow = 4 * half + ((lane & 15) >> 2);
     const int vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
@@ -83,13 +74,14 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
         voff[c] = (uint32_t)(r * p.slot_stride + G::value_slot(r, lane % PPR) * 8) * 2;
     }
 
-    for (long long x = x0; x < x1;) {
-        const Tile t = same_in_all(find_tile<false>(a, x));
-        const int k0 = (int)(x - t.at), k1 = (int)(min(x1, t.at + t.units) - t.at);
-        x = t.at + k1;
+    for (long long x = piece.x0; x < piece.x1;) {
+        const Tile t = line.find(x);
+        const Part part(piece, t, x);
+        const int k0 = part.k0, k1 = part.k1;
+        x = t.at + BEGIN + t.units;
+        if (k0 >= k1) continue;
         int row, head, token;
-        const bool mine = chunk_row<G::ROWS>(a, t, wave * 32 + l32, row, head, token);
-        if (!mine) {                                       // (the sequence's last row again, never stored)
+        if (!tile_row<CHUNKS, G::ROWS>(a, t, wave * 32 + l32, row, head, token)) {   // (the sequence's last row again, never stored)
             token = t.s.n - 1;
             head = p.G - 1;
             row = t.s.row0 + token;
@@ -103,12 +95,17 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
         const int last16 = (t.s.len - 1) & ~15;
         const int32_t* table = p.table + t.b * p.table_stride;
         const long long head_at = t.kvh * p.head_stride;
-        // lanes 0 .. 3: the pages of a unit's 16-key groups (behind the end: the last group again, whose keys nobody sees there)
-        auto pages_of = [&](int u) { return table[min(u * G::KEYS + (lane & 3) * 16, last16) >> p.lg]; };
-        auto bad_of = [&](int pg) { return (int)(__builtin_amdgcn_ballot_w64(pg < 0 || pg >= p.pages) & 15); };
+        // pages of 16 units, a lane per group of 16 keys (behind the end: the last group again, whose keys nobody sees there); the even sixteens and the odd ones
+        auto pages_of = [&](int sixteen) { return table[min((sixteen * 64 + lane) * 16, last16) >> p.lg]; };
+        int even = pages_of((k0 >> 4) + ((k0 >> 4) & 1)), odd = pages_of(k0 >> 4 | 1);
+        auto pages_at = [&](int u) { return (u >> 4) & 1 ? odd : even; };
+        auto bad_of = [&](int u) {
+            const int pg = pages_at(u);
+            return (int)(__builtin_amdgcn_ballot_w64(pg < 0 || pg >= p.pages) >> ((u & 15) * 4)) & 15;
+        };
         // the wave's 16 rows of unit u's keys or values
-        auto issue = [&](const void* from, const uint32_t (&off)[PIECES], bool values, int u, int pg) {
-            const int page = __builtin_amdgcn_readlane(pg, wave), pos = min(u * G::KEYS + wave * 16, last16);
+        auto issue = [&](const void* from, const uint32_t (&off)[PIECES], bool values, int u) {
+            const int page = __builtin_amdgcn_readlane(pages_at(u), (u & 15) * 4 + wave), pos = min(u * G::KEYS + wave * 16, last16);
             const bool ok = page >= 0 && page < p.pages;
             char* to = (values ? vbuf : kbuf) + (u & 1) * G::STAGE + wave * 32 * DH;
             const uint16_t* src = reinterpret_cast<const uint16_t*>(from) + page * p.page_stride + (pos & ((1 << p.lg) - 1)) * p.slot_stride + head_at;
@@ -144,12 +141,11 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
         float m_run = -INFINITY, l_run = 0.f;              // of query l32; the sum over this half's keys
-        int pg0 = pages_of(k0), pg1 = pages_of(k0 + 1), pg2 = pages_of(k0 + 2);       // of units u, u + 1, u + 2
         __syncthreads();                                   // the tile before is done with LDS
-        issue(p.K, koff, false, k0, pg0);
-        issue(p.V, voff, true, k0, pg0);
+        issue(p.K, koff, false, k0);
+        issue(p.V, voff, true, k0);
         landed();
-        if (k0 + 1 < k1) issue(p.K, koff, false, k0 + 1, pg1);
+        if (k0 + 1 < k1) issue(p.K, koff, false, k0 + 1);
         {   // S^T of the first unit
             const char* kc = kbuf + (k0 & 1) * G::STAGE;
 #pragma unroll
@@ -165,14 +161,16 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
                 for (int b = 0; b < 2; ++b) s[b] = mfma32(kf[ks % 3][b], qf[ks], s[b]);
             }
         }
-        for (int u = k0; u < k1; ++u) {
+        // one unit: s are its scores, s2 becomes the next one's
+        auto step = [&](int u, f32x16 (&s)[2], f32x16 (&s2)[2]) {
             landed();                                      // keys of u + 1, values of u
-            if (u + 2 < k1) issue(p.K, koff, false, u + 2, pg2);
-            if (u + 1 < k1) issue(p.V, voff, true, u + 1, pg1);
-            const int bad = bad_of(pg0);
-            pg0 = pg1;
-            pg1 = pg2;
-            pg2 = pages_of(u + 3);
+            if (u + 2 < k1) issue(p.K, koff, false, u + 2);
+            if (u + 1 < k1) issue(p.V, voff, true, u + 1);
+            const int bad = bad_of(u);
+            if ((u & 15) == 6) {                           // (nobody asks for the sixteen before this one any more)
+                const int next = pages_of((u >> 4) + 1);
+                if ((u >> 4) & 1) even = next; else odd = next;
+            }
             // ---- weights in base 2 against a reference that moves when it is passed by more than 10
             const int key0 = u * G::KEYS;
             if (key0 + G::KEYS > all_see || bad) {         // (the same for the wave)
@@ -234,58 +232,52 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
                     const u32x2 v1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsAt)(vc + r1 * DH * 2 + G::value_slot(r1, 4 * i + vpiece) * 16)));
                     acc_o[i] = mfma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, pf[j], acc_o[i]);
                 }
-#pragma unroll
-            for (int b = 0; b < 2; ++b) s[b] = s2[b];
+        };
+        for (int u = k0; u < k1; u += 2) {
+            step(u, s, s2);
+            if (u + 1 == k1) break;
+            step(u + 1, s2, s);
         }
-        const float l = sum_over_halves(l_run);
-        if (k0 == 0 && k1 == t.units) {
+        float l = sum_over_halves(l_run);
+        int again = wave * 32 + l32;
+        asm volatile("" : "+v"(again));                    // (found anew: kept over the loop it would cost registers)
+        const bool mine = tile_row<CHUNKS, G::ROWS>(a, t, again, row, head, token);
+        if (part.whole(t)) {
             if (mine) store_rows<DH>(a, t, row, head, half, acc_o, l > 0.f ? 1.f / l : 0.f);
-        } else {
-            const long long slot = 2LL * me + (k0 == 0 ? 1 : 0);
-            float* po = a.part_o + (slot * G::WAVES + wave) * (32 * DH) + lane;
-#pragma unroll
-            for (int i = 0; i < NB; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) po[(i * 16 + e) * 64] = acc_o[i][e];
-            if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + ((slot * G::WAVES + wave) * 32 + l32) * 2) = f32x2{m_run, l};
+            continue;
         }
-    }
-}
-
-// Puts a cut tile together, see k_paged_join.
-template <int DH>
-__global__ __launch_bounds__(256) void k_paged_tile_join(AttendArgs a) {
-    using G = TileGeom<DH>;
-    constexpr int NB = G::NB;
-    const int W = gridDim.x, me = blockIdx.x, lane = threadIdx.x & 63, l32 = lane & 31, wave = threadIdx.x >> 6;
-    const long long total = line_length<false>(a), x0 = me * total / W, x1 = (me + 1) * total / W;
-    if (x0 >= x1 || x1 >= total) return;
-    const Tile t = find_tile<false>(a, x1 - 1);
-    const long long end = t.at + t.units;
-    if (end == x1 || t.at < x0) return;
-    int last = me;
-    while ((last + 1) * total / W < end) ++last;
-    int row, head, token;
-    const bool mine = chunk_row<G::ROWS>(a, t, wave * 32 + l32, row, head, token);
-    float m = -INFINITY, l = 0.f;
-    f32x16 o[NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    for (int w = me; w <= last; ++w) {
-        if (w > me && w * total / W == (w + 1) * total / W) continue;
-        const long long slot = 2LL * w + (w == me ? 1 : 0);
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + ((slot * G::WAVES + wave) * 32 + l32) * 2);
-        const float mn = fmaxf(m, ml[0]);
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), fw = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - mn);
-        m = mn;
-        l = l * f + ml[1] * fw;
-        const float* po = a.part_o + (slot * G::WAVES + wave) * (32 * DH) + lane;
+        const long long slot = part.slot(piece);
+        float* po = a.part_o + (slot * G::WAVES + wave) * (32 * DH) + 2 * lane;
 #pragma unroll
         for (int i = 0; i < NB; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[i][e] = o[i][e] * f + po[(i * 16 + e) * 64] * fw;
+            for (int e = 0; e < 16; e += 2) put(po + (i * 16 + e) * 64, acc_o[i][e], acc_o[i][e + 1]);
+        if (half == 0) put(a.part_ml + ((slot * G::WAVES + wave) * 32 + l32) * 2, m_run, l);
+        int first, last;
+        if (!comes_last(a, piece, t, first, last, reinterpret_cast<int*>(lds + 4 * G::STAGE))) continue;
+        float m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
+        for (int w = first; w <= last; ++w) {
+            const long long s2 = (2LL * w + (w == first ? 1 : 0)) * G::WAVES + wave;
+            const f32x2 ml = get(a.part_ml + (s2 * 32 + l32) * 2);
+            const float mn = fmaxf(m, ml[0]);
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), fw = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - mn);
+            m = mn;
+            l = l * f + ml[1] * fw;
+            const float* from = a.part_o + s2 * (32 * DH) + 2 * lane;
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const f32x2 v = get(from + (i * 16 + e) * 64);
+                    acc_o[i][e] = acc_o[i][e] * f + v[0] * fw;
+                    acc_o[i][e + 1] = acc_o[i][e + 1] * f + v[1] * fw;
+                }
+        }
+        if (mine) store_rows<DH>(a, t, row, head, half, acc_o, l > 0.f ? 1.f / l : 0.f);
     }
-    if (mine) store_rows<DH>(a, t, row, head, lane >> 5, o, l > 0.f ? 1.f / l : 0.f);
 }

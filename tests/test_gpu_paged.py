@@ -86,8 +86,9 @@ def test_attention_is_the_same_on_every_run(pa):
     ws = pa.paged_workspace(cache, chunk, c.H)
     first = pa.ada_attention_paged(cache, chunk, c.Q.cuda(), ws=ws)["out"]
     for fill in (0, 255):
-        ws.fill_(fill)                                     # nothing is expected of a workspace
+        ws[pa.PAGED_ZERO_BYTES:].fill_(fill)               # nothing is expected of the rest of a workspace
         assert torch.equal(first, pa.ada_attention_paged(cache, chunk, c.Q.cuda(), ws=ws)["out"])
+        assert bool((ws[:pa.PAGED_ZERO_BYTES] == 0).all())
 
 
 def test_pages_outside_the_pool_count_as_masked(pa):
@@ -513,7 +514,7 @@ def test_no_rows(pa):
     c = ref.Case("bf16", 2, 1, 64, 16, [0, 0], [5, 0])
     cache, _ = c.on_gpu(pa)
     chunk = pa.Chunk(c.table.cuda(), c.start.cuda(), c.past_t.cuda(), rows=0)
-    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(1 << 26, dtype=torch.uint8, device="cuda")
     some = torch.zeros(1, 128, dtype=torch.bfloat16, device="cuda")
     assert pa.ada_attention_paged(cache, chunk, some, ws=ws)["status"].item() == OK
     chunk = pa.Chunk(c.table.cuda(), c.start.cuda(), c.past_t.cuda(), rows=1)      # one row, nobody's
