@@ -587,11 +587,11 @@ struct AttendWs { size_t tiles, prefix, tile, part_o, part_ml, bytes; };
 inline bool takes_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G >= 48; }
 
 inline int rows_pieces() { return 4 * ada_hook_cus() < ADA_PAGED_ZERO_BYTES / 4 ? 4 * ada_hook_cus() : ADA_PAGED_ZERO_BYTES / 4; }
-inline int tile_pieces(int d_h) { return (d_h > 128 ? 1 : 2) * ada_hook_cus(); }
+inline int tile_pieces(int d_h) { (void)d_h; return ada_hook_cus() < rows_pieces() ? ada_hook_cus() : rows_pieces(); }
 
 inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
     const size_t tiles = (size_t)((long long)p.rows * p.G / TILE_ROWS + p.B);
-    const size_t rows = (size_t)rows_pieces() * TILE_ROWS, tile_rows = takes_tiles(p, dtype) ? (size_t)tile_pieces(d_h) * 128 : 0;
+    const size_t rows = (size_t)rows_pieces() * TILE_ROWS, tile_rows = takes_tiles(p, dtype) ? (size_t)tile_pieces(d_h) * 256 : 0;
     const size_t parts = 2 * (rows > tile_rows ? rows : tile_rows);           // rows of cut tiles (listed pages always take 16-row ones)
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     AttendWs w;
@@ -606,11 +606,11 @@ inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
 
 // A kernel that needs more LDS than a launch gets unasked.
 template <typename Kernel>
-hipError_t launch_pieces(Kernel kernel, std::once_flag& once, hipError_t& attr_err, int pieces, int lds, const AttendArgs& a, hipStream_t st) {
+hipError_t launch_pieces(Kernel kernel, std::once_flag& once, hipError_t& attr_err, int pieces, int threads, int lds, const AttendArgs& a, hipStream_t st) {
     std::call_once(once, [&] { attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds); });
     if (attr_err != hipSuccess) return attr_err;
     ProfHook ps(ADA_K_ATTN, st);
-    hipLaunchKernelGGL(kernel, dim3(pieces), dim3(256), lds, st, a);
+    hipLaunchKernelGGL(kernel, dim3(pieces), dim3(threads), lds, st, a);
     return hipGetLastError();
 }
 
@@ -618,14 +618,14 @@ template <typename In, int DH, int MODE>
 hipError_t launch_rows(const AttendArgs& a, hipStream_t st) {
     static std::once_flag once;
     static hipError_t attr_err = hipSuccess;
-    return launch_pieces(&k_paged_rows<In, DH, MODE>, once, attr_err, rows_pieces(), rows_lds<In, DH>(), a, st);
+    return launch_pieces(&k_paged_rows<In, DH, MODE>, once, attr_err, rows_pieces(), 256, rows_lds<In, DH>(), a, st);
 }
 
 template <int DH>
 hipError_t launch_tiles(const AttendArgs& a, hipStream_t st) {
     static std::once_flag once;
     static hipError_t attr_err = hipSuccess;
-    return launch_pieces(&k_paged_tile<DH>, once, attr_err, tile_pieces(DH), TileGeom<DH>::LDS, a, st);
+    return launch_pieces(&k_paged_tile<DH>, once, attr_err, tile_pieces(DH), 64 * TileGeom<DH>::WAVES, TileGeom<DH>::LDS, a, st);
 }
 
 template <typename In, int DH>
@@ -645,7 +645,7 @@ hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
     if (!chunks && (long long)a.p.longest * a.p.G <= TILE_ROWS) return launch_rows<In, DH, TOKENS>(a, st);
     {
         ProfHook ps(ADA_K_ATTN, st);
-        hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, chunks ? 128 : TILE_ROWS, chunks ? 64 : UNIT, prefix, tile, tiles);
+        hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, chunks ? TileGeom<DH>::ROWS : TILE_ROWS, chunks ? TileGeom<DH>::KEYS : UNIT, prefix, tile, tiles);
     }
     if (hipError_t e = hipGetLastError()) return e;
     if constexpr (dtype == ADA_BF16)

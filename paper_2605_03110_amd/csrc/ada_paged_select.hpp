@@ -101,7 +101,7 @@ __global__ __launch_bounds__(512) void k_select_pages(SelectArgs a) {
         const int stop = min(end_row, max(s.row0 + s.n, row0 + 1));            // this sequence's rows of the workgroup
         if (row0 < s.row0 || row0 >= s.row0 + s.n) { row0 = row0 + 1; continue; }
         const int n_tok = stop - row0, first_pos = s.past + row0 - s.row0;
-        const int n_pages = ((p.causal ? first_pos + n_tok : s.len) - 1 >> p.lg) + 1;        // that the last of them sees
+        const int n_pages = (((p.causal ? first_pos + n_tok : s.len) - 1) >> p.lg) + 1;        // that the last of them sees
         const int32_t* table = p.table + b * p.table_stride;
         // ---- scores, 16 pages x 16 (token, head) at a time
         float largest_bound = 0.f;

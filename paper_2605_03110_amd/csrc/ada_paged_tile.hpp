@@ -12,9 +12,11 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s16x4* LdsAt;
 
 template <int DH> struct TileGeom {
-    static constexpr int WAVES = 4, ROWS = 32 * WAVES, KEYS = 64, KS = DH / 16, NB = DH / 32, PPR = DH / 8;
+    static constexpr int WAVES = DH > 128 ? 4 : 8, ROWS = 32 * WAVES, KEYS = 64, KS = DH / 16, NB = DH / 32, PPR = DH / 8;
+    static constexpr int KB = KEYS / 32, GROUPS = KEYS / 16, SPAN = 64 / GROUPS;        // blocks of 32 keys and groups of 16 in a unit; units whose groups' pages a wave holds
+    static constexpr bool AHEAD = true;               // the next unit's scores beside this one's weights, where registers allow it
     static constexpr int STAGE = KEYS * DH * 2, LDS = 4 * STAGE + 16;          // keys and values, twice; comes_last's word
-    static constexpr int PER_CU = DH > 128 ? 1 : 2;
+    static constexpr int PER_CU = 1;
     __device__ static int key_slot(int row, int piece) { return piece ^ (row & (PPR >= 16 ? 15 : 7)); }
     __device__ static int value_slot(int row, int piece) { return piece ^ (PPR >= 16 ? (row & 3) << 2 : ((row >> 1) & 1) << 2); }
 };
@@ -51,9 +53,9 @@ __device__ inline void load_to_lds(const void* base, uint32_t off, char* to) {
 }
 
 template <int DH>
-__global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(AttendArgs a) {
+__global__ __launch_bounds__(64 * TileGeom<DH>::WAVES, TileGeom<DH>::PER_CU * TileGeom<DH>::WAVES / 4) void k_paged_tile(AttendArgs a) {
     using G = TileGeom<DH>;
-    constexpr int KS = G::KS, NB = G::NB, PPR = G::PPR, PIECES = DH / 32;      // PIECES: 1 KB loads of a wave's 16 rows
+    constexpr int KS = G::KS, NB = G::NB, PPR = G::PPR, KB = G::KB, MINE = G::KEYS / G::WAVES, PIECES = MINE * DH * 2 / 1024;      // a wave loads MINE rows, 1 KB at a time
     extern __shared__ __align__(16) char lds[];
     char* kbuf = lds;
     char* vbuf = lds + 2 * G::STAGE;
@@ -66,10 +68,11 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
     // where this lane's columns of a value row start in LDS for the transposed reads: rows 4 half + (lane & 15) / 4 + 8 n, columns 16 ((lane >> 4) & 1) + 4 (lane & 3)
     const int vrow = 4 * half + ((lane & 15) >> 2);
     const int vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    uint32_t koff[PIECES], voff[PIECES];                   // where this lane reads in 16 whole rows
+    const int row16 = (wave * MINE) & 15;                  // the wave's first row in its group of 16
+    uint32_t koff[PIECES], voff[PIECES];                   // where this lane reads in a whole group
 #pragma unroll
     for (int c = 0; c < PIECES; ++c) {
-        const int r = c * (512 / DH) + lane / PPR;
+        const int r = row16 + c * (512 / DH) + lane / PPR;
         koff[c] = (uint32_t)(r * p.slot_stride + G::key_slot(r, lane % PPR) * 8) * 2;
         voff[c] = (uint32_t)(r * p.slot_stride + G::value_slot(r, lane % PPR) * 8) * 2;
     }
@@ -95,19 +98,20 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
         const int last16 = (t.s.len - 1) & ~15;
         const int32_t* table = p.table + t.b * p.table_stride;
         const long long head_at = t.kvh * p.head_stride;
-        // pages of 16 units, a lane per group of 16 keys (behind the end: the last group again, whose keys nobody sees there); the even sixteens and the odd ones
-        auto pages_of = [&](int sixteen) { return table[min((sixteen * 64 + lane) * 16, last16) >> p.lg]; };
-        int even = pages_of((k0 >> 4) + ((k0 >> 4) & 1)), odd = pages_of(k0 >> 4 | 1);
-        auto pages_at = [&](int u) { return (u >> 4) & 1 ? odd : even; };
+        // pages of SPAN units, a lane per group of 16 keys (behind the end: the last group again, whose keys nobody sees there); the even spans and the odd ones
+        auto pages_of = [&](int span) { return table[min((span * 64 + lane) * 16, last16) >> p.lg]; };
+        int even = pages_of(k0 / G::SPAN + ((k0 / G::SPAN) & 1)), odd = pages_of(k0 / G::SPAN | 1);
+        auto pages_at = [&](int u) { return (u / G::SPAN) & 1 ? odd : even; };
         auto bad_of = [&](int u) {
             const int pg = pages_at(u);
-            return (int)(__builtin_amdgcn_ballot_w64(pg < 0 || pg >= p.pages) >> ((u & 15) * 4)) & 15;
+            return (int)(__builtin_amdgcn_ballot_w64(pg < 0 || pg >= p.pages) >> (u % G::SPAN * G::GROUPS)) & ((1 << G::GROUPS) - 1);
         };
-        // the wave's 16 rows of unit u's keys or values
+        // the wave's rows of unit u's keys or values
         auto issue = [&](const void* from, const uint32_t (&off)[PIECES], bool values, int u) {
-            const int page = __builtin_amdgcn_readlane(pages_at(u), (u & 15) * 4 + wave), pos = min(u * G::KEYS + wave * 16, last16);
+            const int group = wave * MINE / 16, page = __builtin_amdgcn_readlane(pages_at(u), u % G::SPAN * G::GROUPS + group);
+            const int pos = min(u * G::KEYS + group * 16, last16);
             const bool ok = page >= 0 && page < p.pages;
-            char* to = (values ? vbuf : kbuf) + (u & 1) * G::STAGE + wave * 32 * DH;
+            char* to = (values ? vbuf : kbuf) + (u & 1) * G::STAGE + wave * MINE * DH * 2;
             const uint16_t* src = reinterpret_cast<const uint16_t*>(from) + page * p.page_stride + (pos & ((1 << p.lg) - 1)) * p.slot_stride + head_at;
             if (ok && pos + 16 <= t.s.len) {
 #pragma unroll
@@ -121,7 +125,7 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
             }
 #pragma unroll
             for (int c = 0; c < PIECES; ++c) {
-                const int r = c * (512 / DH) + lane / PPR, in = ok ? min(r, t.s.len - 1 - pos) : 0;
+                const int r = row16 + c * (512 / DH) + lane / PPR, in = ok ? min(r, t.s.len - 1 - pos) : 0;
                 load_to_lds(src, (uint32_t)(in * p.slot_stride + (values ? G::value_slot(r, lane % PPR) : G::key_slot(r, lane % PPR)) * 8) * 2, to + c * 1024);
             }
         };
@@ -129,27 +133,17 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
             __builtin_amdgcn_s_waitcnt(0x0070);
             asm volatile("s_barrier" ::: "memory");
         };
-        u32x4 kf[3][2];                                    // keys, read two steps ahead of their products
+        u32x4 kf[3][KB];                                   // keys, read two steps ahead of their products
         auto read_k = [&](const char* kc, int ks) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < KB; ++b)
                 kf[ks % 3][b] = *reinterpret_cast<const u32x4*>(kc + (b * 32 + l32) * DH * 2 + G::key_slot(l32, 2 * ks + half) * 16);
         };
-        f32x16 acc_o[NB], s[2], s2[2];
+        // S^T of unit u, `beside` what goes between its products
+        auto scores = [&](int u, f32x16 (&s)[KB], auto beside) {
+            const char* kc = kbuf + (u & 1) * G::STAGE;
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
-        float m_run = -INFINITY, l_run = 0.f;              // of query l32; the sum over this half's keys
-        __syncthreads();                                   // the tile before is done with LDS
-        issue(p.K, koff, false, k0);
-        issue(p.V, voff, true, k0);
-        landed();
-        if (k0 + 1 < k1) issue(p.K, koff, false, k0 + 1);
-        {   // S^T of the first unit
-            const char* kc = kbuf + (k0 & 1) * G::STAGE;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < KB; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
             read_k(kc, 0);
@@ -158,24 +152,40 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
             for (int ks = 0; ks < KS; ++ks) {
                 if (ks + 2 < KS) read_k(kc, ks + 2);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) s[b] = mfma32(kf[ks % 3][b], qf[ks], s[b]);
+                for (int b = 0; b < KB; ++b) s[b] = mfma32(kf[ks % 3][b], qf[ks], s[b]);
+                beside(ks);
             }
+        };
+        f32x16 acc_o[NB], s[KB], s2[KB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
+        float m_run = -INFINITY, l_run = 0.f;              // of query l32; the sum over this half's keys
+        __syncthreads();                                   // the tile before is done with LDS
+        issue(p.K, koff, false, k0);
+        issue(p.V, voff, true, k0);
+        if constexpr (G::AHEAD) {
+            landed();
+            if (k0 + 1 < k1) issue(p.K, koff, false, k0 + 1);
+            scores(k0, s, [](int) {});
         }
-        // one unit: s are its scores, s2 becomes the next one's
-        auto step = [&](int u, f32x16 (&s)[2], f32x16 (&s2)[2]) {
-            landed();                                      // keys of u + 1, values of u
-            if (u + 2 < k1) issue(p.K, koff, false, u + 2);
+        // one unit: s are its scores, s2 becomes the next one's (AHEAD)
+        auto step = [&](int u, f32x16 (&s)[KB], f32x16 (&s2)[KB]) {
+            landed();                                      // keys (AHEAD: of u + 1) and values
+            if (u + 1 + G::AHEAD < k1) issue(p.K, koff, false, u + 1 + G::AHEAD);
             if (u + 1 < k1) issue(p.V, voff, true, u + 1);
             const int bad = bad_of(u);
-            if ((u & 15) == 6) {                           // (nobody asks for the sixteen before this one any more)
-                const int next = pages_of((u >> 4) + 1);
-                if ((u >> 4) & 1) even = next; else odd = next;
+            if (u % G::SPAN == 6) {                        // (nobody asks for the span before this one any more)
+                const int next = pages_of(u / G::SPAN + 1);
+                if ((u / G::SPAN) & 1) even = next; else odd = next;
             }
+            if constexpr (!G::AHEAD) scores(u, s, [](int) {});
             // ---- weights in base 2 against a reference that moves when it is passed by more than 10
             const int key0 = u * G::KEYS;
             if (key0 + G::KEYS > all_see || bad) {         // (the same for the wave)
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < KB; ++b)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int k = b * 32 + (e & 3) + 8 * (e >> 2) + 4 * half;
@@ -184,7 +194,7 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
             }
             float mx = -INFINITY;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < KB; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[b][e]);
             mx = max_over_halves(mx) * a.sc2;
@@ -199,44 +209,54 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
                     for (int e = 0; e < 16; ++e) acc_o[i][e] *= f;
             }
             const float m_use = m_run == -INFINITY ? 0.f : m_run;
-            // ---- S^T of the next unit beside the weights of this one (behind the last unit: of what lies in LDS, for nobody)
-            const char* kc = kbuf + ((u + 1) & 1) * G::STAGE;
-            u32x4 pf[4];                                   // weights, one bf16 number each, by 16 keys
+            u32x4 pf[2 * KB];                              // weights, one bf16 number each, by 16 keys
+            auto weights = [&](int w) {                    // the w-th pair
+                const int b = w >> 3, e = 2 * (w & 7);
+                const float w0 = __builtin_amdgcn_exp2f(s[b][e] * a.sc2 - m_use), w1 = __builtin_amdgcn_exp2f(s[b][e + 1] * a.sc2 - m_use);
+                l_run += w0 + w1;
+                pf[2 * b + (e >> 3)][(e & 7) >> 1] = bf16_pair(w0, w1);
+            };
+            if constexpr (G::AHEAD)                        // (behind the last unit: scores of what lies in LDS, for nobody)
+                scores(u + 1, s2, [&](int ks) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                    for (int w = ks * 8 * KB / KS; w < (ks + 1) * 8 * KB / KS; ++w) weights(w);
+                });
+            else
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s2[b][e] = 0.f;
-            read_k(kc, 0);
-            read_k(kc, 1);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                if (ks + 2 < KS) read_k(kc, ks + 2);
-#pragma unroll
-                for (int b = 0; b < 2; ++b) s2[b] = mfma32(kf[ks % 3][b], qf[ks], s2[b]);
-#pragma unroll
-                for (int w = ks * 16 / KS; w < (ks + 1) * 16 / KS; ++w) {
-                    const int b = w >> 3, e = 2 * (w & 7);
-                    const float w0 = __builtin_amdgcn_exp2f(s[b][e] * a.sc2 - m_use), w1 = __builtin_amdgcn_exp2f(s[b][e + 1] * a.sc2 - m_use);
-                    l_run += w0 + w1;
-                    pf[2 * b + (e >> 3)][(e & 7) >> 1] = bf16_pair(w0, w1);
-                }
-            }
+                for (int w = 0; w < 8 * KB; ++w) weights(w);
             // ---- O^T += V^T P^T
             const char* vc = vbuf + (u & 1) * G::STAGE + 8 * (lane & 1);
+            constexpr int NV = 2 * KB * NB, VA = 3;        // products; how many of their operands are read ahead
+            u32x2 vf[VA + 1][2];
+            auto read_v = [&](int n) {
+                const int r0 = 16 * (n / NB) + vrow, r1 = r0 + 8, piece = 4 * (n % NB) + vpiece;
+                vf[n % (VA + 1)][0] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsAt)(vc + r0 * DH * 2 + G::value_slot(r0, piece) * 16)));
+                vf[n % (VA + 1)][1] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsAt)(vc + r1 * DH * 2 + G::value_slot(r1, piece) * 16)));
+            };
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int n = 0; n < VA; ++n) read_v(n);
 #pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    const int r0 = 16 * j + vrow, r1 = r0 + 8;
-                    const u32x2 v0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsAt)(vc + r0 * DH * 2 + G::value_slot(r0, 4 * i + vpiece) * 16)));
-                    const u32x2 v1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsAt)(vc + r1 * DH * 2 + G::value_slot(r1, 4 * i + vpiece) * 16)));
-                    acc_o[i] = mfma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, pf[j], acc_o[i]);
-                }
+            for (int n = 0; n < NV; ++n) {
+                if (n + VA < NV) read_v(n + VA);
+                const u32x2 v0 = vf[n % (VA + 1)][0], v1 = vf[n % (VA + 1)][1];
+                acc_o[n % NB] = mfma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, pf[n / NB], acc_o[n % NB]);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * VA, 1);
+#pragma unroll
+            for (int n = 0; n < NV - VA; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, VA, 1);
         };
-        for (int u = k0; u < k1; u += 2) {
-            step(u, s, s2);
-            if (u + 1 == k1) break;
-            step(u + 1, s2, s);
+        if constexpr (G::AHEAD) {
+            for (int u = k0; u < k1; u += 2) {
+                step(u, s, s2);
+                if (u + 1 == k1) break;
+                step(u + 1, s2, s);
+            }
+        } else {
+            for (int u = k0; u < k1; ++u) step(u, s, s);
         }
         float l = sum_over_halves(l_run);
         int again = wave * 32 + l32;
@@ -257,27 +277,32 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
         if (!comes_last(a, piece, t, first, last, reinterpret_cast<int*>(lds + 4 * G::STAGE))) continue;
         float m = -INFINITY;
         l = 0.f;
+        for (int w = first; w <= last; ++w) m = fmaxf(m, get(a.part_ml + (((2LL * w + (w == first ? 1 : 0)) * G::WAVES + wave) * 32 + l32) * 2)[0]);
+        uint16_t* to = reinterpret_cast<uint16_t*>(a.out) + row * a.ld_out + (long long)(t.kvh * p.G + head) * DH + 4 * half;
+#pragma unroll 1
+        for (int i = 0; i < NB; ++i) {                     // 32 columns at a time: the other registers stay the loop's
+            float o[16];
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
-        for (int w = first; w <= last; ++w) {
-            const long long s2 = (2LL * w + (w == first ? 1 : 0)) * G::WAVES + wave;
-            const f32x2 ml = get(a.part_ml + (s2 * 32 + l32) * 2);
-            const float mn = fmaxf(m, ml[0]);
-            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), fw = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - mn);
-            m = mn;
-            l = l * f + ml[1] * fw;
-            const float* from = a.part_o + s2 * (32 * DH) + 2 * lane;
-#pragma unroll
-            for (int i = 0; i < NB; ++i)
+            for (int e = 0; e < 16; ++e) o[e] = 0.f;
+            l = 0.f;
+            for (int w = first; w <= last; ++w) {
+                const long long s2 = (2LL * w + (w == first ? 1 : 0)) * G::WAVES + wave;
+                const f32x2 ml = get(a.part_ml + (s2 * 32 + l32) * 2);
+                const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
+                l += ml[1] * f;
+                const float* from = a.part_o + s2 * (32 * DH) + 2 * lane + i * 16 * 64;
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
-                    const f32x2 v = get(from + (i * 16 + e) * 64);
-                    acc_o[i][e] = acc_o[i][e] * f + v[0] * fw;
-                    acc_o[i][e + 1] = acc_o[i][e + 1] * f + v[1] * fw;
+                    const f32x2 v = get(from + e * 64);
+                    o[e] += v[0] * f;
+                    o[e + 1] += v[1] * f;
                 }
+            }
+            const float f = l > 0.f ? 1.f / l : 0.f;
+            if (mine)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    *reinterpret_cast<u32x2*>(to + 32 * i + 8 * w) = u32x2{bf16_pair(o[4 * w] * f, o[4 * w + 1] * f), bf16_pair(o[4 * w + 2] * f, o[4 * w + 3] * f)};
         }
-        if (mine) store_rows<DH>(a, t, row, head, half, acc_o, l > 0.f ? 1.f / l : 0.f);
     }
 }
