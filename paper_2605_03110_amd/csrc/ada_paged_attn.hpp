@@ -587,11 +587,11 @@ struct AttendWs { size_t tiles, prefix, tile, part_o, part_ml, bytes; };
 inline bool takes_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G >= 48; }
 
 inline int rows_pieces() { return 4 * ada_hook_cus() < ADA_PAGED_ZERO_BYTES / 4 ? 4 * ada_hook_cus() : ADA_PAGED_ZERO_BYTES / 4; }
-inline int tile_pieces(int d_h) { (void)d_h; return ada_hook_cus() < rows_pieces() ? ada_hook_cus() : rows_pieces(); }
+inline int tile_pieces(int d_h) { const int n = (d_h > 128 ? 1 : 2) * ada_hook_cus(); return n < rows_pieces() ? n : rows_pieces(); }
 
 inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
     const size_t tiles = (size_t)((long long)p.rows * p.G / TILE_ROWS + p.B);
-    const size_t rows = (size_t)rows_pieces() * TILE_ROWS, tile_rows = takes_tiles(p, dtype) ? (size_t)tile_pieces(d_h) * 256 : 0;
+    const size_t rows = (size_t)rows_pieces() * TILE_ROWS, tile_rows = takes_tiles(p, dtype) ? (size_t)tile_pieces(d_h) * 128 : 0;
     const size_t parts = 2 * (rows > tile_rows ? rows : tile_rows);           // rows of cut tiles (listed pages always take 16-row ones)
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     AttendWs w;

@@ -12,11 +12,10 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s16x4* LdsAt;
 
 template <int DH> struct TileGeom {
-    static constexpr int WAVES = DH > 128 ? 4 : 8, ROWS = 32 * WAVES, KEYS = 64, KS = DH / 16, NB = DH / 32, PPR = DH / 8;
+    static constexpr int WAVES = 4, ROWS = 32 * WAVES, KEYS = 64, KS = DH / 16, NB = DH / 32, PPR = DH / 8;
     static constexpr int KB = KEYS / 32, GROUPS = KEYS / 16, SPAN = 64 / GROUPS;        // blocks of 32 keys and groups of 16 in a unit; units whose groups' pages a wave holds
-    static constexpr bool AHEAD = true;               // the next unit's scores beside this one's weights, where registers allow it
     static constexpr int STAGE = KEYS * DH * 2, LDS = 4 * STAGE + 16;          // keys and values, twice; comes_last's word
-    static constexpr int PER_CU = 1;
+    static constexpr int PER_CU = DH > 128 ? 1 : 2;        // workgroups of a CU at once
     __device__ static int key_slot(int row, int piece) { return piece ^ (row & (PPR >= 16 ? 15 : 7)); }
     __device__ static int value_slot(int row, int piece) { return piece ^ (PPR >= 16 ? (row & 3) << 2 : ((row >> 1) & 1) << 2); }
 };
@@ -53,7 +52,7 @@ __device__ inline void load_to_lds(const void* base, uint32_t off, char* to) {
 }
 
 template <int DH>
-__global__ __launch_bounds__(64 * TileGeom<DH>::WAVES, TileGeom<DH>::PER_CU * TileGeom<DH>::WAVES / 4) void k_paged_tile(AttendArgs a) {
+__global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(AttendArgs a) {
     using G = TileGeom<DH>;
     constexpr int KS = G::KS, NB = G::NB, PPR = G::PPR, KB = G::KB, MINE = G::KEYS / G::WAVES, PIECES = MINE * DH * 2 / 1024;      // a wave loads MINE rows, 1 KB at a time
     extern __shared__ __align__(16) char lds[];
@@ -62,6 +61,7 @@ __global__ __launch_bounds__(64 * TileGeom<DH>::WAVES, TileGeom<DH>::PER_CU * Ti
     const PagedArgs& p = a.p;
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool young = blockIdx.x >= gridDim.x / 2;
     const Line<CHUNKS> line(a);
     if (line.total == 0) return;
     const Piece piece(line.total);
@@ -165,22 +165,24 @@ __global__ __launch_bounds__(64 * TileGeom<DH>::WAVES, TileGeom<DH>::PER_CU * Ti
         __syncthreads();                                   // the tile before is done with LDS
         issue(p.K, koff, false, k0);
         issue(p.V, voff, true, k0);
-        if constexpr (G::AHEAD) {
-            landed();
-            if (k0 + 1 < k1) issue(p.K, koff, false, k0 + 1);
-            scores(k0, s, [](int) {});
-        }
-        // one unit: s are its scores, s2 becomes the next one's (AHEAD)
+        landed();
+        if (k0 + 1 < k1) issue(p.K, koff, false, k0 + 1);
+        scores(k0, s, [](int) {});
+        // one unit: s are its scores, s2 becomes the next one's
         auto step = [&](int u, f32x16 (&s)[KB], f32x16 (&s2)[KB]) {
-            landed();                                      // keys (AHEAD: of u + 1) and values
-            if (u + 1 + G::AHEAD < k1) issue(p.K, koff, false, u + 1 + G::AHEAD);
+            // Of two workgroups on a CU the older one is served first and ends a sixth earlier; the younger one goes first in every other unit
+            // (8192 tokens: 600 and 715 us -> alike, 644 -> 628 us a call)
+            if (G::PER_CU > 1 && young) {
+                if (u & 1) __builtin_amdgcn_s_setprio(0); else __builtin_amdgcn_s_setprio(1);
+            }
+            landed();                                      // keys of u + 1, values of u
+            if (u + 2 < k1) issue(p.K, koff, false, u + 2);
             if (u + 1 < k1) issue(p.V, voff, true, u + 1);
             const int bad = bad_of(u);
             if (u % G::SPAN == 6) {                        // (nobody asks for the span before this one any more)
                 const int next = pages_of(u / G::SPAN + 1);
                 if ((u / G::SPAN) & 1) even = next; else odd = next;
             }
-            if constexpr (!G::AHEAD) scores(u, s, [](int) {});
             // ---- weights in base 2 against a reference that moves when it is passed by more than 10
             const int key0 = u * G::KEYS;
             if (key0 + G::KEYS > all_see || bad) {         // (the same for the wave)
@@ -216,14 +218,10 @@ __global__ __launch_bounds__(64 * TileGeom<DH>::WAVES, TileGeom<DH>::PER_CU * Ti
                 l_run += w0 + w1;
                 pf[2 * b + (e >> 3)][(e & 7) >> 1] = bf16_pair(w0, w1);
             };
-            if constexpr (G::AHEAD)                        // (behind the last unit: scores of what lies in LDS, for nobody)
-                scores(u + 1, s2, [&](int ks) {
+            scores(u + 1, s2, [&](int ks) {                // (behind the last unit: of what lies in LDS, for nobody)
 #pragma unroll
-                    for (int w = ks * 8 * KB / KS; w < (ks + 1) * 8 * KB / KS; ++w) weights(w);
-                });
-            else
-#pragma unroll
-                for (int w = 0; w < 8 * KB; ++w) weights(w);
+                for (int w = ks * 8 * KB / KS; w < (ks + 1) * 8 * KB / KS; ++w) weights(w);
+            });
             // ---- O^T += V^T P^T
             const char* vc = vbuf + (u & 1) * G::STAGE + 8 * (lane & 1);
             constexpr int NV = 2 * KB * NB, VA = 3;        // products; how many of their operands are read ahead
@@ -249,14 +247,10 @@ __global__ __launch_bounds__(64 * TileGeom<DH>::WAVES, TileGeom<DH>::PER_CU * Ti
             }
             __builtin_amdgcn_sched_group_barrier(0x008, VA, 1);
         };
-        if constexpr (G::AHEAD) {
-            for (int u = k0; u < k1; u += 2) {
-                step(u, s, s2);
-                if (u + 1 == k1) break;
-                step(u + 1, s2, s);
-            }
-        } else {
-            for (int u = k0; u < k1; ++u) step(u, s, s);
+        for (int u = k0; u < k1; u += 2) {
+            step(u, s, s2);
+            if (u + 1 == k1) break;
+            step(u + 1, s2, s);
         }
         float l = sum_over_halves(l_run);
         int again = wave * 32 + l32;
