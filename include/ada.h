@@ -417,8 +417,8 @@ typedef struct {
  * Two sequences may share pages that are only read.  A page that a call appends to belongs to one sequence.
  */
 
-/* Bytes of workspace that ada_attention_paged and ada_attention_pages need for these sizes (256-byte aligned).  0 for arguments that those
- * calls refuse.  The first ADA_PAGED_ZERO_BYTES of it must be zero before the first use (ada_workspace_init on them, or any memset); every
+/* Bytes of workspace that the calls below that take one need for these sizes (256-byte aligned).  0 for arguments that they
+ * refuse.  The first ADA_PAGED_ZERO_BYTES of it must be zero before the first use (ada_workspace_init on them, or any memset); every
  * call leaves them so.  Calls that share a workspace must not overlap in time; one that is abandoned part-way needs it cleared again. */
 #define ADA_PAGED_ZERO_BYTES 8192
 size_t ada_paged_workspace_bytes(const ada_paged_cache* cache, const ada_paged_chunk* chunk, int H);
@@ -466,7 +466,8 @@ int ada_attention_paged(const ada_paged_cache* cache, const ada_paged_chunk* chu
  */
 #define ADA_SELECT_MAX_PAGES 8192
 int ada_select_pages(const ada_paged_cache* cache, const ada_paged_chunk* chunk, const void* Q, int H, int64_t ldq,
-                     int budget, int first, int last, int32_t* pages, int32_t* counts, int32_t* status, void* stream, unsigned flags);
+                     int budget, int first, int last, int32_t* pages, int32_t* counts, int32_t* status, void* ws, size_t ws_bytes,
+                     void* stream, unsigned flags);
 
 /*
  * ada_attention_paged with s in the pages that are listed for the row and its head of the cache only (ada_select_pages' outputs, or any

@@ -103,7 +103,8 @@ SCRATCH_BUDGET = {
     "k_paged_tileI": 0,
     "k_cache_appendI": 0,
     "k_cache_boundsI": 0,
-    "k_select_pagesI": 0,
+    "k_select_scoresI": 0,
+    "k_select_chooseI": 0,
 }
 
 
@@ -242,7 +243,7 @@ def lib():
         L.ada_attention_paged.restype = i32
         L.ada_attention_paged.argtypes = [cp, kp, vp, i32, i64, vp, i64, vp, vp, sz, vp, u32]
         L.ada_select_pages.restype = i32
-        L.ada_select_pages.argtypes = [cp, kp, vp, i32, i64, i32, i32, i32, vp, vp, vp, vp, u32]
+        L.ada_select_pages.argtypes = [cp, kp, vp, i32, i64, i32, i32, i32, vp, vp, vp, vp, sz, vp, u32]
         L.ada_attention_pages.restype = i32
         L.ada_attention_pages.argtypes = [cp, kp, vp, i32, i64, vp, vp, i32, vp, i64, vp, vp, sz, vp, u32]
         L.ada_assign_nearest.restype = i32
@@ -764,7 +765,7 @@ def ada_paged_workspace_bytes(cache: PagedCache, chunk: Chunk, H: int) -> int:
 
 
 def paged_workspace(cache: PagedCache, chunk: Chunk, H: int) -> torch.Tensor:
-    """A workspace for ada_attention_paged and ada_attention_pages of these sizes, ready for use."""
+    """A workspace for the paged calls on these sizes, ready for use."""
     n = ada_paged_workspace_bytes(cache, chunk, H)
     if n == 0:
         raise ValueError("sizes that no paged attention takes")
@@ -875,7 +876,7 @@ def ada_select_pages(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, budget: i
                      status: Optional[torch.Tensor] = None, stream=None, flags: int = 0) -> Dict[str, torch.Tensor]:
     """For every row and head of the cache the `budget` pages of its sequence that its queries may weigh most, by the pages' bounds; the
     `first` and `last` pages it sees are always among them.  Returns pages [rows, H_kv, budget] int32 (ascending, -1 behind the last), counts
-    [rows, H_kv] int32 (`out`'s, if given) and status.  No workspace is needed; `ws` is taken so that the paged calls look alike."""
+    [rows, H_kv] int32 (`out`'s, if given) and status."""
     H = _paged_rows(cache, chunk, Q, "Q")
     if cache.bounds is None:
         raise ValueError("the cache has no bounds to score pages by")
@@ -886,12 +887,13 @@ def ada_select_pages(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, budget: i
     _check_lists(cache, chunk, out["pages"], out["counts"])
     if out["pages"].shape[2] != int(budget):
         raise ValueError("pages must have `budget` entries per row and head")
+    ws = paged_workspace(cache, chunk, H) if ws is None else ws
     with _on(cache, chunk):
         rc = lib().ada_select_pages(cache.ref, chunk.ref, _ptr(Q), H, _ld(Q), int(budget), int(first), int(last), _ptr(out["pages"]),
-                                    _ptr(out["counts"]), _ptr(status), _stream(stream), int(flags))
+                                    _ptr(out["counts"]), _ptr(status), _ptr(ws), ws.numel(), _stream(stream), int(flags))
     if rc != OK:
         raise AdaError(rc, "ada_select_pages")
-    return dict(pages=out["pages"], counts=out["counts"], status=status, _keep=(cache, chunk, Q))
+    return dict(pages=out["pages"], counts=out["counts"], status=status, _keep=(cache, chunk, Q, ws))
 
 
 def ada_attention_pages(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, pages: torch.Tensor, counts: torch.Tensor, *,

@@ -164,7 +164,9 @@ size_t ada_paged_workspace_bytes(const ada_paged_cache* cache, const ada_paged_c
     PagedArgs a;
     int32_t unused = 0;
     if (paged_args(cache, chunk, H, &unused, 0, a) != ADA_OK) return 0;
-    return attend_ws(a, cache->d_h, cache->dtype).bytes;
+    const size_t attention = attend_ws(a, cache->d_h, cache->dtype).bytes;
+    const size_t selection = a.bounds && a.max_pages <= ADA_SELECT_MAX_PAGES ? ADA_PAGED_ZERO_BYTES + select_ws(a).bytes : 0;
+    return attention > selection ? attention : selection;
 }
 
 int ada_cache_append(const ada_paged_cache* cache, const ada_paged_chunk* chunk, const void* Q, int64_t ldq, const void* K,
@@ -204,17 +206,19 @@ int ada_attention_pages(const ada_paged_cache* cache, const ada_paged_chunk* chu
 }
 
 int ada_select_pages(const ada_paged_cache* cache, const ada_paged_chunk* chunk, const void* Q, int H, int64_t ldq, int budget,
-                     int first, int last, int32_t* pages, int32_t* counts, int32_t* status, void* stream, unsigned flags) {
+                     int first, int last, int32_t* pages, int32_t* counts, int32_t* status, void* ws, size_t ws_bytes, void* stream,
+                     unsigned flags) {
     SelectArgs a;
     if (int e = paged_args(cache, chunk, H, status, flags, a.p)) return e;
-    if (!cache->bounds || !Q || !pages || !counts) return ADA_ERR_NULL;
+    if (!cache->bounds || !Q || !pages || !counts || !ws) return ADA_ERR_NULL;
     if (!rows_ok(Q, ldq, (int64_t)H * cache->d_h, elem_size(cache->dtype))) return ADA_ERR_SHAPE;
     if (budget < 1 || budget > MAX_TOKENS / 256 || first < 0 || last < 0 || first > budget || last > budget - first) return ADA_ERR_SHAPE;
     if (chunk->max_pages > ADA_SELECT_MAX_PAGES) return ADA_ERR_SHAPE;
+    if (ws_bytes < ADA_PAGED_ZERO_BYTES + select_ws(a.p).bytes || (uintptr_t)ws % 256) return ADA_ERR_WORKSPACE;
     if (chunk->rows == 0) return ADA_OK;
     a.Q = Q; a.ldq = ldq; a.budget = budget; a.first = first; a.last = last; a.list = pages; a.count = counts;
     return paged_dispatch(cache->dtype, cache->d_h, [&](auto in, auto dh) {
-        return launch_select<decltype(in), decltype(dh)::value>(a, (hipStream_t)stream);
+        return launch_select<decltype(in), decltype(dh)::value>(a, ws, (hipStream_t)stream);
     });
 }
 

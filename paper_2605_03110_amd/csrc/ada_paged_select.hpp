@@ -6,7 +6,9 @@
 // largest and one below tau - 2 E is not; for those between, where they are more than the places left, the sum is taken again in fp64.
 //   E = (2 d_h + 16) 2^-24 max_h |q_h|_1 max |bound|: at most 2 d_h roundings, each of no more than the sum of the products' magnitudes (and 16 to
 //   spare for the bound's own arithmetic).
-// A workgroup takes `tokens` rows and one head of the cache; each of its waves scores 16 pages at a time, then a wave chooses for a token.
+// Two launches: scores, a wave per 16 pages and some rows, to the workspace as integers in the numbers' order; then a wave per row and head of the cache
+// that chooses.  (In one launch, scores in LDS: a workgroup per row was 33 us for 16 tokens at 20 to 32 thousand keys, most CUs without work, and 83 for
+// 2048 tokens at 8 thousand.)
 #pragma once
 
 struct SelectArgs {
@@ -15,7 +17,11 @@ struct SelectArgs {
     long long ldq;
     int budget, first, last;
     int32_t *list, *count;
-    int lg_heads, tokens, slots;                           // columns of a product: 2^lg_heads heads (a group of up to 16, or a part of it) x tokens; pages that LDS has room for
+    int row0, rows;                                        // the rows of this pair of launches
+    int lg_heads;                                          // columns of a product: 2^lg_heads heads (a group of up to 16, or a part of it) x tokens
+    int slots;                                             // pages per row and head in the workspace: whole sixteens
+    uint32_t* key;                                         // [rows][H_kv][slots], 0: no such page
+    float* most;                                           // [rows][H_kv][slots / 16] largest |bound| of sixteen pages
 };
 
 __device__ inline uint32_t ordered(float f) {              // as unsigned integers in the order of the numbers; never 0
@@ -28,21 +34,60 @@ __device__ inline unsigned long long ordered(double f) {
     return u ^ ((u >> 63) ? ~0ull : 1ull << 63);
 }
 
-// The largest t with at least k of the n keys >= t (0 < k <= keys that are not 0): the k-th largest key, or, where that leaves exactly
-// k of them, something between it and the next one.
-template <typename Key, typename Get>
-__device__ inline Key kth_largest(int n, int k, Get&& get) {
-    const int lane = threadIdx.x & 63;
-    Key t = 0;
-    for (int bit = (int)sizeof(Key) * 8 - 1; bit >= 0; --bit) {
-        const Key with = t | ((Key)1 << bit);
-        int c = 0;
-        for (int i0 = 0; i0 < n; i0 += 64) c += __popcll(__builtin_amdgcn_ballot_w64(i0 + lane < n && get(min(i0 + lane, n - 1)) >= with));
-        if (c >= k) t = with;
-        if (c == k) break;
+// n keys, a lane's every 64th; up to 512 are held in registers, more are asked for again each time (0: no key).
+template <typename Key, typename Get> struct Keys {
+    static constexpr int HELD = 8;
+    const Get& get;
+    int n;
+    Key held[HELD];
+    __device__ __forceinline__ Keys(int count, const Get& g) : get(g), n(count) { block(0, held); }
+    __device__ __forceinline__ void block(int i0, Key (&k)[HELD]) const {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const int at = i0 + i * 64 + lane;
+            k[i] = i0 + i * 64 < n && at < n ? get(at) : 0;
+        }
     }
-    return t;
-}
+    template <typename F> __device__ __forceinline__ void each(F&& f) const {                  // f(first key's number, block of keys)
+        f(0, held);
+        for (int i0 = 64 * HELD; i0 < n; i0 += 64 * HELD) {
+            Key k[HELD];
+            block(i0, k);
+            f(i0, k);
+        }
+    }
+    __device__ __forceinline__ int count(Key from) const {                 // keys >= from (> 0)
+        int c = 0;
+        each([&](int i0, const Key (&k)[HELD]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) if (i0 + i * 64 < n) c += __popcll(__builtin_amdgcn_ballot_w64(k[i] >= from));
+        });
+        return c;
+    }
+    // The k-th largest key (0 < k <= keys)
+    __device__ __forceinline__ Key kth(int k) const {
+        Key t = 0;
+        for (int bit = (int)sizeof(Key) * 8 - 1; bit >= 0; --bit) {
+            const Key with = t | ((Key)1 << bit);
+            const int c = count(with);
+            if (c >= k) t = with;
+            if (c == k) break;                             // (the k largest are those >= t: the smallest of them is meant)
+        }
+        Key least = ~(Key)0;
+        each([&](int, const Key (&key)[HELD]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) if (key[i] >= t && key[i] < least) least = key[i];
+        });
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const Key other = __shfl_xor(least, o, 64);
+            if (other < least) least = other;
+        }
+        return least;
+    }
+};
+template <typename Key, typename Get> __device__ inline Keys<Key, Get> keys_of(int n, const Get& get) { return Keys<Key, Get>(n, get); }
 
 template <typename In> __device__ inline u32x4 part(u32x4 w, bool negative);   // the negative entries, or the others; 0 elsewhere
 template <> __device__ inline u32x4 part<uint16_t>(u32x4 w, bool negative) {
@@ -79,207 +124,293 @@ template <typename In> __device__ inline double as_double(In v);
 template <> __device__ inline double as_double<uint16_t>(uint16_t v) { return (double)__uint_as_float((uint32_t)v << 16); }
 template <> __device__ inline double as_double<float>(float v) { return (double)v; }
 
-__host__ __device__ inline size_t select_lds(int tokens, int slots) { return (size_t)tokens * slots * 12 + 16 * 4 + 64 * 4; }
-
+// Scores: a workgroup takes 64 pages (a wave 16), `per_group` rows and a head of the cache.
 template <typename In, int DH>
-__global__ __launch_bounds__(512) void k_select_pages(SelectArgs a) {
+__global__ __launch_bounds__(256) void k_select_scores(SelectArgs a, int per_group) {
     constexpr int EPP = 16 / (int)sizeof(In), KF = DH / (4 * EPP);
-    extern __shared__ __align__(16) char lds[];
     const PagedArgs& p = a.p;
-    double* exact_of = reinterpret_cast<double*>(lds);                         // [tokens][slots]
-    uint32_t* key_of = reinterpret_cast<uint32_t*>(exact_of + a.tokens * a.slots);   // [tokens][slots]; 0: no such page
-    float* qsum = reinterpret_cast<float*>(key_of + a.tokens * a.slots);       // [16] max_h |q_h|_1 of a token
-    float* most = qsum + 16;                                                   // [waves] max |bound|
-    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4, waves = blockDim.x >> 6;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kvh = blockIdx.y, end_row = min((int)(blockIdx.x + 1) * a.tokens, p.rows);
-    const int per = 1 << a.lg_heads;
-    for (int row0 = blockIdx.x * a.tokens; row0 < end_row;) {
-        const int b = paged_find(p, row0);
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kvh = blockIdx.z;
+    const int j0 = blockIdx.x * 64 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 16;
+    const int per = 1 << a.lg_heads, tokens = 16 >> a.lg_heads;                // columns: a token's heads side by side
+    const int end = min((int)(blockIdx.y + 1) * per_group, a.rows) + a.row0;
+    for (int row = blockIdx.y * per_group + a.row0; row < end;) {
+        const int b = paged_find(p, row);
         if (b >= p.B) return;                                                  // rows behind the last sequence
         const Seq s = paged_seq(p, b);
-        const int stop = min(end_row, max(s.row0 + s.n, row0 + 1));            // this sequence's rows of the workgroup
-        if (row0 < s.row0 || row0 >= s.row0 + s.n) { row0 = row0 + 1; continue; }
-        const int n_tok = stop - row0, first_pos = s.past + row0 - s.row0;
-        const int n_pages = (((p.causal ? first_pos + n_tok : s.len) - 1) >> p.lg) + 1;        // that the last of them sees
-        const int32_t* table = p.table + b * p.table_stride;
-        // ---- scores, 16 pages x 16 (token, head) at a time
-        float largest_bound = 0.f;
-        for (int h0 = 0; h0 < p.G; h0 += 16) {                                 // (groups of more than 16 heads in turns)
-            const int tok = min(l16 >> a.lg_heads, n_tok - 1), head = h0 + min(l16 & (per - 1), min(p.G - h0, 16) - 1);
-            const In* q = reinterpret_cast<const In*>(a.Q) + (row0 + tok) * a.ldq + (long long)(kvh * p.G + head) * DH;
-            u32x4 qf[KF];
-            float q1 = 0.f;
+        if (row < s.row0 || row >= s.row0 + s.n) { ++row; continue; }
+        const int stop = min(end, s.row0 + s.n);                               // this sequence's rows
+        const int n_pages = (((p.causal ? s.past + stop - s.row0 : s.len) - 1) >> p.lg) + 1;  // that the last of them sees
+        if (j0 >= n_pages) { row = stop; continue; }
+        const int page = p.table[b * p.table_stride + min(j0 + l16, n_pages - 1)];
+        const bool there = page >= 0 && page < p.pages;
+        if (!there) raise(p, ADA_ERR_INDEX);
+        const In* low = reinterpret_cast<const In*>(p.bounds) + ((long long)(there ? page : 0) * p.H_kv + kvh) * 2 * DH;
+        u32x4 kf[2][KF];
 #pragma unroll
-            for (int c = 0; c < KF; ++c) {
-                qf[c] = *reinterpret_cast<const u32x4*>(q + (c * 4 + g) * EPP);
-                q1 += abs_sum<In>(qf[c]);
-            }
-            q1 = sum_over_groups(q1);
-            for (int o = 1; o < per; o <<= 1) q1 = fmaxf(q1, __shfl_xor(q1, o, 64));
-            if (wave == 0 && g == 0 && (l16 & (per - 1)) == 0 && (l16 >> a.lg_heads) < n_tok)
-                qsum[l16 >> a.lg_heads] = h0 ? fmaxf(qsum[l16 >> a.lg_heads], q1) : q1;
-            for (int j0 = wave * 16; j0 < n_pages; j0 += waves * 16) {
-                const int j = min(j0 + l16, n_pages - 1), page = table[j];
-                const bool there = page >= 0 && page < p.pages;
-                if (!there) raise(p, ADA_ERR_INDEX);
-                const In* low = reinterpret_cast<const In*>(p.bounds) + ((long long)(there ? page : 0) * p.H_kv + kvh) * 2 * DH;
+        for (int side = 0; side < 2; ++side)
+#pragma unroll
+            for (int c = 0; c < KF; ++c) kf[side][c] = *reinterpret_cast<const u32x4*>(low + side * DH + (c * 4 + g) * EPP);
+        float most = 0.f;
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+#pragma unroll
+            for (int c = 0; c < KF; ++c) most = fmaxf(most, largest<In>(kf[side][c]));
+        most = there ? most : 0.f;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+        const unsigned long long known = __builtin_amdgcn_ballot_w64(there);  // bit l16: page j0 + l16
+        const int tok = l16 >> a.lg_heads, sub = l16 & (per - 1);
+        auto query = [&](int r, int h0) {
+            return reinterpret_cast<const In*>(a.Q) + min(r + tok, stop - 1) * a.ldq + (long long)(kvh * p.G + h0 + min(sub, min(p.G - h0, 16) - 1)) * DH + g * EPP;
+        };
+        u32x4 qf[KF];
+        auto fetch = [&](const In* q) {
+#pragma unroll
+            for (int c = 0; c < KF; ++c) qf[c] = *reinterpret_cast<const u32x4*>(q + c * 4 * EPP);
+        };
+        fetch(query(row, 0));
+        for (; row < stop; row += tokens) {
+            float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            for (int h0 = 0; h0 < p.G; h0 += 16) {                             // (groups of more than 16 heads in turns)
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-                float m = 0.f;
 #pragma unroll
-                for (int side = 0; side < 2; ++side) {
-                    u32x4 kf[KF];
-#pragma unroll
-                    for (int c = 0; c < KF; ++c) kf[c] = *reinterpret_cast<const u32x4*>(low + side * DH + (c * 4 + g) * EPP);
+                for (int side = 0; side < 2; ++side)
 #pragma unroll
                     for (int c = 0; c < KF; ++c) {
-                        m = fmaxf(m, largest<In>(kf[c]));
                         const u32x4 qs = part<In>(qf[c], side == 0);
-                        if constexpr (sizeof(In) == 2) acc = mfma16(kf[c], qs, acc);
+                        if constexpr (sizeof(In) == 2) acc = mfma16(kf[side][c], qs, acc);
                         else
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[c][e]), __uint_as_float(qs[e]), acc, 0, 0, 0);
+                                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[side][c][e]), __uint_as_float(qs[e]), acc, 0, 0, 0);
                     }
-                }
-                if (there) largest_bound = fmaxf(largest_bound, m);
-                const unsigned long long known = __builtin_amdgcn_ballot_w64(there);          // bit l16: page j0 + l16
+                const bool more = h0 + 16 < p.G;
+                if (more || row + tokens < stop) fetch(query(more ? row : row + tokens, more ? h0 + 16 : 0));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = acc[e];
-                    for (int o = 1; o < per; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-                    const int at = 4 * g + e, t = l16 >> a.lg_heads;
-                    if ((l16 & (per - 1)) == 0 && t < n_tok && j0 + at < n_pages) {
-                        uint32_t* to = key_of + t * a.slots + j0 + at;
-                        const uint32_t k = (known >> at) & 1 ? ordered(v) : 0u;
-                        *to = h0 ? max(*to, k) : k;
-                    }
-                }
+                for (int e = 0; e < 4; ++e) best[e] = fmaxf(best[e], acc[e]);
+            }
+            u32x4 key;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float v = best[e];
+                for (int o = 1; o < per; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+                key[e] = (known >> (4 * g + e)) & 1 ? ordered(v) : 0u;
+            }
+            if (sub == 0 && row + tok < stop) {
+                const long long at = ((long long)(row + tok - a.row0) * p.H_kv + kvh) * a.slots + j0;
+                *reinterpret_cast<u32x4*>(a.key + at + 4 * g) = key;
+                if (g == 0) a.most[at >> 4] = most;
             }
         }
-        for (int o = 1; o < 64; o <<= 1) largest_bound = fmaxf(largest_bound, __shfl_xor(largest_bound, o, 64));
-        if (lane == 0) most[wave] = largest_bound;
-        __syncthreads();
-        // ---- choice, a wave per token
-        for (int t = wave; t < n_tok; t += waves) {
-            const int row = row0 + t, have = ((p.causal ? first_pos + t : s.len - 1) >> p.lg) + 1;
-            const uint32_t* key = key_of + t * a.slots;
-            double* exact = exact_of + t * a.slots;
-            const int lo = min(a.first, have), hi = max(lo, have - a.last), free = a.budget - lo - (have - hi);      // candidates lo .. hi - 1
-            uint32_t all_from = 1, between_from = 1;       // chosen: keys >= all_from; and of those >= between_from the exact ones below
-            unsigned long long exact_from = 0;
-            int ties = 0;                                  // of those equal to exact_from, the first so many
-            int there = 0;
-            for (int i0 = lo; i0 < hi; i0 += 64) there += __popcll(__builtin_amdgcn_ballot_w64(i0 + lane < hi && key[min(i0 + lane, hi - 1)] != 0u));
-            if (there > free) {
-                if (free <= 0) all_from = between_from = 0xFFFFFFFFu;          // (no key is that large)
-                else {
-                    const uint32_t from = kth_largest<uint32_t>(hi - lo, free, [&](int i) { return key[lo + i]; });
-                    uint32_t least = 0xFFFFFFFFu;          // the k-th largest key itself
-                    for (int i = lo + lane; i < hi; i += 64) if (key[i] >= from) least = min(least, key[i]);
-                    for (int o = 1; o < 64; o <<= 1) least = min(least, (uint32_t)__shfl_xor((int)least, o, 64));
-                    float bound = 0.f;
-                    for (int w = 0; w < waves; ++w) bound = fmaxf(bound, most[w]);
-                    const float tau = unordered(least), err = (2 * DH + 16) * 5.9604645e-8f * qsum[t] * bound * 2.02f;
-                    between_from = max(ordered(tau - err), 1u);
-                    const uint32_t above = ordered(tau + err);
-                    int sure = 0, open = 0;
-                    for (int i0 = lo; i0 < hi; i0 += 64) {
-                        const uint32_t k = i0 + lane < hi ? key[min(i0 + lane, hi - 1)] : 0u;
-                        sure += __popcll(__builtin_amdgcn_ballot_w64(k > above));
-                        open += __popcll(__builtin_amdgcn_ballot_w64(k >= between_from && k <= above));
-                    }
-                    all_from = above + 1;
-                    const int need = free - sure;
-                    if (open == need) all_from = between_from;
-                    else {
-                        for (int i0 = lo; i0 < hi; i0 += 64) {
-                            const uint32_t k = i0 + lane < hi ? key[min(i0 + lane, hi - 1)] : 0u;
-                            for (unsigned long long left = __builtin_amdgcn_ballot_w64(k >= between_from && k <= above); left; left &= left - 1) {
-                                const int i = i0 + __ffsll(left) - 1;
-                                const In* low = reinterpret_cast<const In*>(p.bounds) + ((long long)table[i] * p.H_kv + kvh) * 2 * DH;
-                                double best = -INFINITY;
-                                for (int h = 0; h < p.G; ++h) {
-                                    const In* q = reinterpret_cast<const In*>(a.Q) + row * a.ldq + (long long)(kvh * p.G + h) * DH;
-                                    double sum = 0.0;
-#pragma unroll
-                                    for (int c = 0; c < DH / 64; ++c) {
-                                        const double x = as_double<In>(q[c * 64 + lane]);
-                                        sum += x * (x < 0.0 ? as_double<In>(low[c * 64 + lane]) : as_double<In>(low[DH + c * 64 + lane]));
-                                    }
-                                    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
-                                    best = sum > best ? sum : best;
-                                }
-                                if (lane == 0) exact[i] = best;
-                            }
-                        }
-                        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                        auto open_key = [&](int i) { return key[lo + i] >= between_from && key[lo + i] <= above ? ordered(exact[lo + i]) : 0ull; };
-                        const unsigned long long efrom = kth_largest<unsigned long long>(hi - lo, need, open_key);
-                        unsigned long long eleast = ~0ull;
-                        for (int i = lane; i < hi - lo; i += 64) {
-                            const unsigned long long k = open_key(i);
-                            if (k != 0ull && k >= efrom && k < eleast) eleast = k;
-                        }
-                        for (int o = 1; o < 64; o <<= 1) {
-                            const unsigned long long k = __shfl_xor(eleast, o, 64);
-                            if (k < eleast) eleast = k;
-                        }
-                        int over = 0;
-                        for (int i0 = 0; i0 < hi - lo; i0 += 64) over += __popcll(__builtin_amdgcn_ballot_w64(i0 + lane < hi - lo && open_key(min(i0 + lane, hi - lo - 1)) > eleast));
-                        exact_from = eleast;
-                        ties = need - over;
-                    }
-                }
-            }
-            // ---- the list
-            int32_t* to = a.list + ((long long)row * p.H_kv + kvh) * a.budget;
-            const unsigned long long below = (1ull << lane) - 1;
-            int n = 0, tied = 0;
-            for (int i0 = 0; i0 < have; i0 += 64) {
-                const int i = i0 + lane, ic = min(i, have - 1);
-                const uint32_t k = key[ic];
-                const bool forced = ic < lo || ic >= hi;
-                bool in = i < have && k != 0u && (forced || k >= all_from), tie = false;
-                if (exact_from != 0ull && i < have && !forced && k < all_from && k >= between_from) {
-                    const unsigned long long e = ordered(exact[ic]);
-                    in = e > exact_from;
-                    tie = e == exact_from;
-                }
-                const unsigned long long ts = __builtin_amdgcn_ballot_w64(tie);
-                if (tie && tied + __popcll(ts & below) < ties) in = true;
-                tied += __popcll(ts);
-                const unsigned long long ins = __builtin_amdgcn_ballot_w64(in);
-                const int place = n + __popcll(ins & below);
-                if (in && place < a.budget) to[place] = i;                     // (scores that are not numbers can let too many in)
-                n = min(n + __popcll(ins), a.budget);
-            }
-            for (int i = n + lane; i < a.budget; i += 64) to[i] = -1;
-            if (lane == 0) a.count[(long long)row * p.H_kv + kvh] = n;
-        }
-        __syncthreads();
-        row0 = stop;
+        row = stop;
     }
 }
 
+// One page's score in fp64, in all lanes: 16 lanes share a head, four heads at a time.
 template <typename In, int DH>
-hipError_t launch_select(SelectArgs a, hipStream_t st) {
+__device__ inline double exact_score(int G, const In* q_row, const In* low) {
+    constexpr int C = DH / 16, W = C * (int)sizeof(In) / 4;                    // columns and 32-bit words of a lane
+    const int lane = threadIdx.x & 63, c0 = (lane & 15) * C;
+    uint32_t lo[W], hi[W];
+    __builtin_memcpy(lo, __builtin_assume_aligned(low + c0, 8), sizeof(lo));
+    __builtin_memcpy(hi, __builtin_assume_aligned(low + DH + c0, 8), sizeof(hi));
+    auto value = [](const uint32_t (&w)[W], int c) {
+        if constexpr (sizeof(In) == 4) return (double)__uint_as_float(w[c]);
+        else return (double)(c & 1 ? bf16_hi(w[c >> 1]) : bf16_lo(w[c >> 1]));
+    };
+    double best = -INFINITY;
+    for (int h0 = 0; h0 < G; h0 += 4) {
+        uint32_t q[W];
+        __builtin_memcpy(q, __builtin_assume_aligned(q_row + (long long)min(h0 + (lane >> 4), G - 1) * DH + c0, 8), sizeof(q));
+        double sum = 0.0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const double x = value(q, c);
+            sum += x * (x < 0.0 ? value(lo, c) : value(hi, c));
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o, 64);
+        best = sum > best ? sum : best;
+    }
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+        const double other = __shfl_xor(best, o, 64);
+        best = other > best ? other : best;
+    }
+    return best;
+}
+
+template <typename In, int DH>
+__global__ __launch_bounds__(256) void k_select_choose(SelectArgs a) {
+    constexpr int EPP = 16 / (int)sizeof(In), LPR = DH / EPP;                  // lanes that read a head
     const PagedArgs& p = a.p;
+    const int lane = threadIdx.x & 63;
+    const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (unit >= a.rows * p.H_kv) return;
+    const int row = a.row0 + unit / p.H_kv, kvh = unit % p.H_kv, b = paged_find(p, row);
+    if (b >= p.B) return;
+    const Seq s = paged_seq(p, b);
+    if (row < s.row0 || row >= s.row0 + s.n) return;
+    const int have = ((p.causal ? s.past + row - s.row0 : s.len - 1) >> p.lg) + 1;
+    const int lo = min(a.first, have), hi = max(lo, have - a.last), free = a.budget - lo - (have - hi);      // candidates lo .. hi - 1
+    const uint32_t* key = a.key + (long long)unit * a.slots;
+    const int32_t* table = p.table + b * p.table_stride;
+    const In* q_row = reinterpret_cast<const In*>(a.Q) + row * a.ldq + (long long)kvh * p.G * DH;
+    int32_t* to = a.list + ((long long)row * p.H_kv + kvh) * a.budget;
+    int n = 0;
+    const unsigned long long below = (1ull << lane) - 1;
+    auto put_out = [&](bool in, int page) __attribute__((always_inline)) {
+        const unsigned long long ins = __builtin_amdgcn_ballot_w64(in);
+        const int place = n + __popcll(ins & below);
+        if (in && place < a.budget) to[place] = page;      // (scores that are not numbers can let too many in)
+        n = min(n + __popcll(ins), a.budget);
+    };
+    auto forced = [&](int from, int end) {
+        for (int i0 = from; i0 < end; i0 += 64) put_out(i0 + lane < end && key[min(i0 + lane, end - 1)] != 0u, i0 + lane);
+    };
+    forced(0, lo);
+    const auto get = [&](int i) { return key[lo + i]; };
+    const auto candidates = keys_of<uint32_t>(hi - lo, get);
+    // chosen: keys >= all_from; of the others from between_from on ("open") those whose exact score is above exact_from, and the first `ties` equal to it
+    uint32_t all_from = 1, between_from = 1;
+    if (candidates.count(1) <= free) {
+        candidates.each([&](int i0, const uint32_t (&k)[8]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i0 + i * 64 < hi - lo) put_out(k[i] != 0u, lo + i0 + i * 64 + lane);
+        });
+    } else if (free > 0) {
+        // what the scores are exact to
+        float q1 = 0.f, most = 0.f;
+        for (int h0 = 0; h0 < p.G; h0 += 64 / LPR) {
+            float sum = abs_sum<In>(*reinterpret_cast<const u32x4*>(q_row + (long long)min(h0 + lane / LPR, p.G - 1) * DH + (lane % LPR) * EPP));
+#pragma unroll
+            for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor(sum, o, 64);
+            q1 = fmaxf(q1, sum);
+        }
+        const float* m = a.most + (long long)unit * (a.slots >> 4);
+        for (int i = lane; i < (have + 15) >> 4; i += 64) most = fmaxf(most, m[i]);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            q1 = fmaxf(q1, __shfl_xor(q1, o, 64));
+            most = fmaxf(most, __shfl_xor(most, o, 64));
+        }
+        const float tau = unordered(candidates.kth(free)), err = (2 * DH + 16) * 5.9604645e-8f * q1 * most * 2.02f;
+        between_from = max(ordered(tau - err), 1u);
+        const uint32_t above = ordered(tau + err);
+        all_from = above + 1;
+        const int sure = candidates.count(all_from), open = candidates.count(between_from) - sure, need = free - sure;
+        auto is_open = [&](uint32_t k) { return k >= between_from && k <= above; };
+        if (open == need) all_from = between_from;
+        if (open == need || open <= 64) {
+            unsigned long long chosen = 0;                 // of the open pages, by their order
+            if (open != need) {
+                unsigned long long mine = 0;               // lane i: the exact score of the i-th
+                int i = 0;
+                candidates.each([&](int i0, const uint32_t (&k)[8]) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int w = 0; w < 8; ++w)
+                        for (unsigned long long left = i0 + w * 64 < hi - lo ? __builtin_amdgcn_ballot_w64(is_open(k[w])) : 0ull; left; left &= left - 1, ++i) {
+                            const int page = lo + i0 + w * 64 + __ffsll(left) - 1;
+                            const double e = exact_score<In, DH>(p.G, q_row, reinterpret_cast<const In*>(p.bounds) + ((long long)table[page] * p.H_kv + kvh) * 2 * DH);
+                            if (lane == i) mine = ordered(e);
+                        }
+                });
+                int taken = 0;                             // one place after the other: the largest left, the first of equal ones
+                for (; taken < need; ++taken) {
+                    unsigned long long top = (chosen >> lane) & 1 ? 0ull : mine;
+#pragma unroll
+                    for (int o = 1; o < 64; o <<= 1) {
+                        const unsigned long long other = __shfl_xor(top, o, 64);
+                        top = other > top ? other : top;
+                    }
+                    const unsigned long long at = __builtin_amdgcn_ballot_w64(mine == top && !((chosen >> lane) & 1));
+                    chosen |= at & (~at + 1);
+                }
+            }
+            int seen = 0;
+            candidates.each([&](int i0, const uint32_t (&k)[8]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    if (i0 + w * 64 >= hi - lo) continue;
+                    const bool o = is_open(k[w]) && k[w] < all_from;
+                    const unsigned long long os = __builtin_amdgcn_ballot_w64(o);
+                    put_out((k[w] != 0u && k[w] >= all_from) || (o && (chosen >> ((seen + __popcll(os & below)) & 63)) & 1), lo + i0 + w * 64 + lane);
+                    seen += __popcll(os);
+                }
+            });
+        } else {
+            // more than 64 within the error of each other (alike pages, queries of zeros): every lane takes the sums of its own pages
+            const auto open_key = [&](int i) {
+                if (!is_open(key[lo + i])) return 0ull;
+                const In* low = reinterpret_cast<const In*>(p.bounds) + ((long long)table[lo + i] * p.H_kv + kvh) * 2 * DH;
+                double best = -INFINITY;
+                for (int h = 0; h < p.G; ++h) {
+                    double sum = 0.0;
+                    for (int c = 0; c < DH; ++c) {
+                        const double x = as_double<In>(q_row[(long long)h * DH + c]);
+                        sum += x * (x < 0.0 ? as_double<In>(low[c]) : as_double<In>(low[DH + c]));
+                    }
+                    best = sum > best ? sum : best;
+                }
+                return ordered(best);
+            };
+            const auto opens = keys_of<unsigned long long>(hi - lo, open_key);
+            const unsigned long long exact_from = opens.kth(need);
+            const int ties = need - opens.count(exact_from + 1);
+            int tied = 0;
+            opens.each([&](int i0, const unsigned long long (&e)[8]) __attribute__((always_inline)) {
+                uint32_t k[8];
+                candidates.block(i0, k);
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    if (i0 + w * 64 >= hi - lo) continue;
+                    const unsigned long long ts = __builtin_amdgcn_ballot_w64(e[w] == exact_from);
+                    put_out(k[w] >= all_from || e[w] > exact_from || (e[w] == exact_from && tied + __popcll(ts & below) < ties), lo + i0 + w * 64 + lane);
+                    tied += __popcll(ts);
+                }
+            });
+        }
+    }
+    forced(hi, have);
+    for (int i = n + lane; i < a.budget; i += 64) to[i] = -1;
+    if (lane == 0) a.count[(long long)row * p.H_kv + kvh] = n;
+}
+
+// ------------------------------------------------------------------------------------------------ host
+struct SelectWs { int slots, rows; size_t most, bytes; };  // rows of one pair of launches
+
+inline SelectWs select_ws(const PagedArgs& p) {
+    SelectWs w;
+    w.slots = (p.max_pages + 15) / 16 * 16;
+    const size_t row = (size_t)p.H_kv * w.slots * 4, most = 64u << 20;        // 64 MB of keys at a time, or a row's
+    w.rows = p.rows;
+    if (row * p.rows > most) w.rows = row < most ? (int)(most / row) : 1;
+    w.most = (row * w.rows + 255) / 256 * 256;
+    w.bytes = w.most + (w.most / 16 + 255) / 256 * 256;
+    return w;
+}
+
+template <typename In, int DH>
+hipError_t launch_select(SelectArgs a, void* ws, hipStream_t st) {
+    const PagedArgs& p = a.p;
+    const SelectWs w = select_ws(p);
     a.lg_heads = 0;
     while ((1 << a.lg_heads) < (p.G < 16 ? p.G : 16)) ++a.lg_heads;
-    a.slots = (p.max_pages + 1) / 2 * 2;
-    // as many tokens as a product has columns for; fewer where their scores would leave room for one workgroup of a CU only
-    a.tokens = p.longest == 1 ? 1 : 16 >> a.lg_heads;
-    while (a.tokens > 1 && select_lds(a.tokens, a.slots) > 65536) a.tokens >>= 1;
-    static std::once_flag once;
-    static hipError_t attr_err = hipSuccess;
-    std::call_once(once, [] {
-        attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_select_pages<In, DH>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)select_lds(1, ADA_SELECT_MAX_PAGES));
-    });
-    if (attr_err != hipSuccess) return attr_err;
-    ProfHook ps(ADA_K_ATTN, st);
-    hipLaunchKernelGGL((k_select_pages<In, DH>), dim3((p.rows + a.tokens - 1) / a.tokens, p.H_kv), dim3(p.longest == 1 ? 512 : 256),
-                       select_lds(a.tokens, a.slots), st, a);
-    return hipGetLastError();
+    a.slots = w.slots;
+    char* at = reinterpret_cast<char*>(ws) + ADA_PAGED_ZERO_BYTES;
+    a.key = reinterpret_cast<uint32_t*>(at);
+    a.most = reinterpret_cast<float*>(at + w.most);
+    const int per_group = p.longest == 1 ? 1 : 64;         // rows that share a wave's pages
+    for (a.row0 = 0; a.row0 < p.rows; a.row0 += a.rows) {
+        a.rows = p.rows - a.row0 < w.rows ? p.rows - a.row0 : w.rows;
+        {
+            ProfHook ps(ADA_K_ATTN, st);
+            hipLaunchKernelGGL((k_select_scores<In, DH>), dim3((w.slots + 63) / 64, (a.rows + per_group - 1) / per_group, p.H_kv), dim3(256), 0, st, a, per_group);
+        }
+        if (hipError_t e = hipGetLastError()) return e;
+        ProfHook ps(ADA_K_ATTN, st);
+        hipLaunchKernelGGL((k_select_choose<In, DH>), dim3((unsigned)(((long long)a.rows * p.H_kv + 3) / 4)), dim3(256), 0, st, a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }

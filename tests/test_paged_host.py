@@ -34,7 +34,7 @@ def calls(ada, cache, chunk, H=4, status=AT, Q=AT, ldq=256):
     L, c, k = ada.lib(), None if cache is None else ctypes.byref(cache), None if chunk is None else ctypes.byref(chunk)
     return (L.ada_cache_append(c, k, Q, ldq, AT, 128, AT, 128, H, None, None, 0.0, None, 0, 0, AT, 256, status, None, 0),
             L.ada_attention_paged(c, k, Q, H, ldq, AT, 256, status, AT, 1 << 40, None, 0),
-            L.ada_select_pages(c, k, Q, H, ldq, 3, 1, 1, AT, AT, status, None, 0),
+            L.ada_select_pages(c, k, Q, H, ldq, 3, 1, 1, AT, AT, status, AT, 1 << 40, None, 0),
             L.ada_attention_pages(c, k, Q, H, ldq, AT, AT, 3, AT, 256, status, AT, 1 << 40, None, 0))
 
 
@@ -85,10 +85,11 @@ def test_single_arguments(ada):
         assert append(**bad) == SHAPE, bad
     assert append(out=None) == NULL and append(Q=None) == NULL
 
-    def pick(budget=3, first=1, last=1, chunk=k, pages=AT, counts=AT):
-        return L.ada_select_pages(c, chunk, AT, 4, 256, budget, first, last, pages, counts, AT, None, 0)
+    def pick(budget=3, first=1, last=1, chunk=k, pages=AT, counts=AT, ws=AT, n=1 << 40):
+        return L.ada_select_pages(c, chunk, AT, 4, 256, budget, first, last, pages, counts, AT, ws, n, None, 0)
     assert pick(budget=0) == SHAPE and pick(first=-1) == SHAPE and pick(last=3) == SHAPE and pick(first=2, last=2) == SHAPE
-    assert pick(pages=None) == NULL and pick(counts=None) == NULL
+    assert pick(pages=None) == NULL and pick(counts=None) == NULL and pick(ws=None) == NULL
+    assert pick(ws=AT + 64) == WS and pick(n=1000) == WS
     assert pick(chunk=ctypes.byref(chunk_of(ada, max_pages=8193, table_stride=8193))) == SHAPE
 
     def attend(ws=AT, n=1 << 40, out=AT, ldo=256):
