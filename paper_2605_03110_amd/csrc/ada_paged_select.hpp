@@ -7,7 +7,7 @@
 //   E = (2 d_h + 16) 2^-24 max_h |q_h|_1 max |bound|: at most 2 d_h roundings, each of no more than the sum of the products' magnitudes (and 16 to
 //   spare for the bound's own arithmetic).
 // Two launches: scores, a wave per 16 pages and some rows, to the workspace as integers in the numbers' order; then a wave per row and head of the cache
-// that chooses.  (In one launch, scores in LDS: a workgroup per row was 33 us for 16 tokens at 20 to 32 thousand keys, most CUs without work, and 83 for
+// that chooses.  (In one launch, scores in LDS: a workgroup per row took 33 us for 16 tokens at 20 to 32 thousand keys, most CUs without work, and 83 for
 // 2048 tokens at 8 thousand.)
 #pragma once
 
@@ -34,13 +34,38 @@ __device__ inline unsigned long long ordered(double f) {
     return u ^ ((u >> 63) ? ~0ull : 1ull << 63);
 }
 
-// n keys, a lane's every 64th; up to 512 are held in registers, more are asked for again each time (0: no key).
-template <typename Key, typename Get> struct Keys {
-    static constexpr int HELD = 8;
+// maximum over lanes 2^lg at a time (neighbours), in all of them
+__device__ __forceinline__ float max_over_neighbours(float v, int lg) {
+    auto with = [&](auto ctrl) { return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), decltype(ctrl)::value, 15, 15, false))); };
+    if (lg > 0) v = with(Const<0xB1>());                   // lane ^ 1
+    if (lg > 1) v = with(Const<0x4E>());                   // lane ^ 2
+    if (lg > 2) v = with(Const<0x141>());                  // the other half of eight, mirrored
+    if (lg > 3) v = with(Const<0x140>());                  // the other half of sixteen, mirrored
+    return v;
+}
+// maximum over the wave
+__device__ __forceinline__ uint32_t max_of_wave(uint32_t v) {
+    auto with = [&](auto ctrl) { return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, 15, 15, false)); };
+    v = with(Const<0xB1>());
+    v = with(Const<0x4E>());
+    v = with(Const<0x141>());
+    v = with(Const<0x140>());
+    auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((uint32_t)a[0], (uint32_t)a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (uint32_t)__builtin_amdgcn_readfirstlane(max((uint32_t)b[0], (uint32_t)b[1]));
+}
+
+// n keys, a lane's every 64th; the first 64 HELD are held in registers, more are asked for again each time (0: no key).
+template <typename Key, int HELD_, typename Get> struct Keys {
+    static constexpr int HELD = HELD_;
     const Get& get;
     int n;
     Key held[HELD];
-    __device__ __forceinline__ Keys(int count, const Get& g) : get(g), n(count) { block(0, held); }
+    __device__ __forceinline__ Keys(int count, const Get& g, const Key (&first)[HELD]) : get(g), n(count) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) held[i] = first[i];
+    }
     __device__ __forceinline__ void block(int i0, Key (&k)[HELD]) const {
         const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -49,7 +74,7 @@ template <typename Key, typename Get> struct Keys {
             k[i] = i0 + i * 64 < n && at < n ? get(at) : 0;
         }
     }
-    template <typename F> __device__ __forceinline__ void each(F&& f) const {                  // f(first key's number, block of keys)
+    template <typename F> __device__ __forceinline__ void each(F&& f) const {  // f(first key's number, block of keys)
         f(0, held);
         for (int i0 = 64 * HELD; i0 < n; i0 += 64 * HELD) {
             Key k[HELD];
@@ -57,7 +82,7 @@ template <typename Key, typename Get> struct Keys {
             f(i0, k);
         }
     }
-    __device__ __forceinline__ int count(Key from) const {                 // keys >= from (> 0)
+    __device__ __forceinline__ int count(Key from) const { // keys >= from (> 0)
         int c = 0;
         each([&](int i0, const Key (&k)[HELD]) __attribute__((always_inline)) {
 #pragma unroll
@@ -68,7 +93,23 @@ template <typename Key, typename Get> struct Keys {
     // The k-th largest key (0 < k <= keys)
     __device__ __forceinline__ Key kth(int k) const {
         Key t = 0;
-        for (int bit = (int)sizeof(Key) * 8 - 1; bit >= 0; --bit) {
+        int bit = (int)sizeof(Key) * 8 - 1;
+        if constexpr (sizeof(Key) == 4) {                  // what the keys have in common in front is known already
+            Key most = 0, least = ~(Key)0;
+            each([&](int, const Key (&key)[HELD]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < HELD; ++i) {
+                    most = max(most, key[i]);
+                    least = min(least, key[i] ? key[i] : ~(Key)0);
+                }
+            });
+            most = max_of_wave(most);
+            least = ~max_of_wave(~least);
+            if (most == least) return most;
+            bit = 31 - __clz(most ^ least);
+            t = bit == 31 ? 0 : most >> (bit + 1) << (bit + 1);
+        }
+        for (; bit >= 0; --bit) {
             const Key with = t | ((Key)1 << bit);
             const int c = count(with);
             if (c >= k) t = with;
@@ -77,8 +118,9 @@ template <typename Key, typename Get> struct Keys {
         Key least = ~(Key)0;
         each([&](int, const Key (&key)[HELD]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < HELD; ++i) if (key[i] >= t && key[i] < least) least = key[i];
+            for (int i = 0; i < HELD; ++i) if (key[i] != 0 && key[i] >= t && key[i] < least) least = key[i];
         });
+        if constexpr (sizeof(Key) == 4) return ~max_of_wave(~least);
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const Key other = __shfl_xor(least, o, 64);
@@ -87,18 +129,22 @@ template <typename Key, typename Get> struct Keys {
         return least;
     }
 };
-template <typename Key, typename Get> __device__ inline Keys<Key, Get> keys_of(int n, const Get& get) { return Keys<Key, Get>(n, get); }
 
-template <typename In> __device__ inline u32x4 part(u32x4 w, bool negative);   // the negative entries, or the others; 0 elsewhere
-template <> __device__ inline u32x4 part<uint16_t>(u32x4 w, bool negative) {
-    const u32x4 m = ((w >> 15) & 0x00010001u) * 0xFFFFu;
-    return negative ? w & m : w & ~m;
+// the negative entries and the others, 0 elsewhere
+template <typename In> __device__ inline void split(u32x4 w, u32x4& negative, u32x4& others);
+template <> __device__ inline void split<uint16_t>(u32x4 w, u32x4& negative, u32x4& others) {
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    const u32x4 m = __builtin_bit_cast(u32x4, __builtin_bit_cast(s16x8, w) >> 15);
+    negative = w & m;
+    others = w & ~m;
 }
-template <> __device__ inline u32x4 part<float>(u32x4 w, bool negative) {
-    u32x4 r;
+template <> __device__ inline void split<float>(u32x4 w, u32x4& negative, u32x4& others) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = ((w[i] >> 31) != 0) == negative ? w[i] : 0u;
-    return r;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t m = (uint32_t)((int)w[i] >> 31);
+        negative[i] = w[i] & m;
+        others[i] = w[i] & ~m;
+    }
 }
 template <typename In> __device__ inline float largest(u32x4 w);               // magnitude
 template <> __device__ inline float largest<uint16_t>(u32x4 w) {
@@ -124,13 +170,13 @@ template <typename In> __device__ inline double as_double(In v);
 template <> __device__ inline double as_double<uint16_t>(uint16_t v) { return (double)__uint_as_float((uint32_t)v << 16); }
 template <> __device__ inline double as_double<float>(float v) { return (double)v; }
 
-// Scores: a workgroup takes 64 pages (a wave 16), `per_group` rows and a head of the cache.
-template <typename In, int DH>
+// Scores: a wave takes 16 SETS pages, `per_group` rows and a head of the cache.  SETS: 2 where rows share pages, as every wave reads the queries again.
+template <typename In, int DH, int SETS>
 __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a, int per_group) {
     constexpr int EPP = 16 / (int)sizeof(In), KF = DH / (4 * EPP);
     const PagedArgs& p = a.p;
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kvh = blockIdx.z;
-    const int j0 = blockIdx.x * 64 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 16;
+    const int j0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 16 * SETS;
     const int per = 1 << a.lg_heads, tokens = 16 >> a.lg_heads;                // columns: a token's heads side by side
     const int end = min((int)(blockIdx.y + 1) * per_group, a.rows) + a.row0;
     for (int row = blockIdx.y * per_group + a.row0; row < end;) {
@@ -141,24 +187,6 @@ __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a, int per_gro
         const int stop = min(end, s.row0 + s.n);                               // this sequence's rows
         const int n_pages = (((p.causal ? s.past + stop - s.row0 : s.len) - 1) >> p.lg) + 1;  // that the last of them sees
         if (j0 >= n_pages) { row = stop; continue; }
-        const int page = p.table[b * p.table_stride + min(j0 + l16, n_pages - 1)];
-        const bool there = page >= 0 && page < p.pages;
-        if (!there) raise(p, ADA_ERR_INDEX);
-        const In* low = reinterpret_cast<const In*>(p.bounds) + ((long long)(there ? page : 0) * p.H_kv + kvh) * 2 * DH;
-        u32x4 kf[2][KF];
-#pragma unroll
-        for (int side = 0; side < 2; ++side)
-#pragma unroll
-            for (int c = 0; c < KF; ++c) kf[side][c] = *reinterpret_cast<const u32x4*>(low + side * DH + (c * 4 + g) * EPP);
-        float most = 0.f;
-#pragma unroll
-        for (int side = 0; side < 2; ++side)
-#pragma unroll
-            for (int c = 0; c < KF; ++c) most = fmaxf(most, largest<In>(kf[side][c]));
-        most = there ? most : 0.f;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-        const unsigned long long known = __builtin_amdgcn_ballot_w64(there);  // bit l16: page j0 + l16
         const int tok = l16 >> a.lg_heads, sub = l16 & (per - 1);
         auto query = [&](int r, int h0) {
             return reinterpret_cast<const In*>(a.Q) + min(r + tok, stop - 1) * a.ldq + (long long)(kvh * p.G + h0 + min(sub, min(p.G - h0, 16) - 1)) * DH + g * EPP;
@@ -169,95 +197,191 @@ __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a, int per_gro
             for (int c = 0; c < KF; ++c) qf[c] = *reinterpret_cast<const u32x4*>(q + c * 4 * EPP);
         };
         fetch(query(row, 0));
+        u32x4 kf[SETS][2][KF];
+        bool there[SETS];
+        unsigned long long known[SETS];                    // bit l16: page j0 + 16 set + l16
+        float most[SETS];
+        const In* low[SETS];
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) {
+            const int page = p.table[b * p.table_stride + min(j0 + i * 16 + l16, n_pages - 1)];
+            there[i] = page >= 0 && page < p.pages;
+            low[i] = reinterpret_cast<const In*>(p.bounds) + ((long long)(there[i] ? page : 0) * p.H_kv + kvh) * 2 * DH;
+        }
+#pragma unroll
+        for (int i = 0; i < SETS; ++i)
+#pragma unroll
+            for (int side = 0; side < 2; ++side)
+#pragma unroll
+                for (int c = 0; c < KF; ++c) kf[i][side][c] = *reinterpret_cast<const u32x4*>(low[i] + side * DH + (c * 4 + g) * EPP);
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) {
+            if (!there[i]) raise(p, ADA_ERR_INDEX);
+            most[i] = 0.f;
+#pragma unroll
+            for (int side = 0; side < 2; ++side)
+#pragma unroll
+                for (int c = 0; c < KF; ++c) most[i] = fmaxf(most[i], largest<In>(kf[i][side][c]));
+            most[i] = __uint_as_float(max_of_wave(__float_as_uint(there[i] ? most[i] : 0.f)));                // (not negative: in the order of their bits)
+            known[i] = __builtin_amdgcn_ballot_w64(there[i]);
+        }
         for (; row < stop; row += tokens) {
-            float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            f32x4 best[SETS];
+#pragma unroll
+            for (int i = 0; i < SETS; ++i) best[i] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
             for (int h0 = 0; h0 < p.G; h0 += 16) {                             // (groups of more than 16 heads in turns)
-                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+                f32x4 part[SETS][2];
 #pragma unroll
-                for (int side = 0; side < 2; ++side)
+                for (int i = 0; i < SETS; ++i) part[i][0] = part[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int c = 0; c < KF; ++c) {
-                        const u32x4 qs = part<In>(qf[c], side == 0);
-                        if constexpr (sizeof(In) == 2) acc = mfma16(kf[side][c], qs, acc);
-                        else
+                for (int c = 0; c < KF; ++c) {
+                    u32x4 qs[2];
+                    split<In>(qf[c], qs[0], qs[1]);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[side][c][e]), __uint_as_float(qs[e]), acc, 0, 0, 0);
-                    }
+                    for (int side = 0; side < 2; ++side)
+#pragma unroll
+                        for (int i = 0; i < SETS; ++i) {
+                            if constexpr (sizeof(In) == 2) part[i][side] = mfma16(kf[i][side][c], qs[side], part[i][side]);
+                            else
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    part[i][side] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][side][c][e]), __uint_as_float(qs[side][e]), part[i][side], 0, 0, 0);
+                        }
+                }
                 const bool more = h0 + 16 < p.G;
                 if (more || row + tokens < stop) fetch(query(more ? row : row + tokens, more ? h0 + 16 : 0));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) best[e] = fmaxf(best[e], acc[e]);
-            }
-            u32x4 key;
+                for (int i = 0; i < SETS; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float v = best[e];
-                for (int o = 1; o < per; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-                key[e] = (known >> (4 * g + e)) & 1 ? ordered(v) : 0u;
+                    for (int e = 0; e < 4; ++e) best[i][e] = fmaxf(best[i][e], part[i][0][e] + part[i][1][e]);
             }
-            if (sub == 0 && row + tok < stop) {
-                const long long at = ((long long)(row + tok - a.row0) * p.H_kv + kvh) * a.slots + j0;
-                *reinterpret_cast<u32x4*>(a.key + at + 4 * g) = key;
-                if (g == 0) a.most[at >> 4] = most;
+#pragma unroll
+            for (int i = 0; i < SETS; ++i) {
+                u32x4 key;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = max_over_neighbours(best[i][e], a.lg_heads);
+                    key[e] = (known[i] >> (4 * g + e)) & 1 ? ordered(v) : 0u;
+                }
+                if (sub == 0 && row + tok < stop && j0 + i * 16 < a.slots) {
+                    const long long at = ((long long)(row + tok - a.row0) * p.H_kv + kvh) * a.slots + j0 + i * 16;
+                    *reinterpret_cast<u32x4*>(a.key + at + 4 * g) = key;
+                    if (g == 0) a.most[at >> 4] = most[i];
+                }
             }
         }
         row = stop;
     }
 }
 
-// One page's score in fp64, in all lanes: 16 lanes share a head, four heads at a time.
+// Scores of four pages in fp64, in all lanes: 16 lanes share a head, four heads at a time.
 template <typename In, int DH>
-__device__ inline double exact_score(int G, const In* q_row, const In* low) {
+__device__ __forceinline__ void exact_scores(int G, const In* q_row, const In* const (&low)[4], double (&best)[4]) {
     constexpr int C = DH / 16, W = C * (int)sizeof(In) / 4;                    // columns and 32-bit words of a lane
     const int lane = threadIdx.x & 63, c0 = (lane & 15) * C;
-    uint32_t lo[W], hi[W];
-    __builtin_memcpy(lo, __builtin_assume_aligned(low + c0, 8), sizeof(lo));
-    __builtin_memcpy(hi, __builtin_assume_aligned(low + DH + c0, 8), sizeof(hi));
+    uint32_t lo[4][W], hi[4][W];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __builtin_memcpy(lo[i], __builtin_assume_aligned(low[i] + c0, 8), sizeof(lo[i]));
+        __builtin_memcpy(hi[i], __builtin_assume_aligned(low[i] + DH + c0, 8), sizeof(hi[i]));
+        best[i] = -INFINITY;
+    }
     auto value = [](const uint32_t (&w)[W], int c) {
         if constexpr (sizeof(In) == 4) return (double)__uint_as_float(w[c]);
         else return (double)(c & 1 ? bf16_hi(w[c >> 1]) : bf16_lo(w[c >> 1]));
     };
-    double best = -INFINITY;
     for (int h0 = 0; h0 < G; h0 += 4) {
         uint32_t q[W];
         __builtin_memcpy(q, __builtin_assume_aligned(q_row + (long long)min(h0 + (lane >> 4), G - 1) * DH + c0, 8), sizeof(q));
-        double sum = 0.0;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const double x = value(q, c);
-            sum += x * (x < 0.0 ? value(lo, c) : value(hi, c));
+        for (int i = 0; i < 4; ++i) {
+            double sum = 0.0;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const double x = value(q, c);
+                sum += x * (x < 0.0 ? value(lo[i], c) : value(hi[i], c));
+            }
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o, 64);
+            best[i] = sum > best[i] ? sum : best[i];
         }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o, 64);
-        best = sum > best ? sum : best;
     }
 #pragma unroll
-    for (int o = 16; o < 64; o <<= 1) {
-        const double other = __shfl_xor(best, o, 64);
-        best = other > best ? other : best;
-    }
-    return best;
+    for (int o = 16; o < 64; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const double other = __shfl_xor(best[i], o, 64);
+            best[i] = other > best[i] ? other : best[i];
+        }
 }
 
-template <typename In, int DH>
-__global__ __launch_bounds__(256) void k_select_choose(SelectArgs a) {
-    constexpr int EPP = 16 / (int)sizeof(In), LPR = DH / EPP;                  // lanes that read a head
+// HELD: 2 where a sequence has up to 128 pages (2048 rows of 8 heads at 8 thousand keys: 35.8 -> 25.3 us), else 8.
+template <typename In, int DH, int HELD>
+__global__ __launch_bounds__(256, HELD == 2 && DH * sizeof(In) <= 256 ? 4 : 2) void k_select_choose(SelectArgs a) {
+    constexpr int EPP = 16 / (int)sizeof(In), LPR = DH / EPP;                  // LPR: lanes that read a head
     const PagedArgs& p = a.p;
     const int lane = threadIdx.x & 63;
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     if (unit >= a.rows * p.H_kv) return;
-    const int row = a.row0 + unit / p.H_kv, kvh = unit % p.H_kv, b = paged_find(p, row);
+    const int row = a.row0 + unit / p.H_kv, kvh = unit % p.H_kv;
+    // asked for before it is known which of it is the row's: the keys that are held, the bounds' sizes, four heads or more of queries
+    const uint32_t* key = a.key + (long long)unit * a.slots;
+    uint32_t raw[HELD];
+#pragma unroll
+    for (int w = 0; w < HELD; ++w) raw[w] = w * 64 + lane < a.slots ? key[w * 64 + lane] : 0u;
+    const float most0 = lane < a.slots >> 4 ? a.most[(long long)unit * (a.slots >> 4) + lane] : 0.f;
+    const In* q_row = reinterpret_cast<const In*>(a.Q) + row * a.ldq + (long long)kvh * p.G * DH;
+    auto size_of = [&](int h0) {                           // |q_h|_1 of heads h0 + lane / LPR
+        float sum = abs_sum<In>(*reinterpret_cast<const u32x4*>(q_row + (long long)min(h0 + lane / LPR, p.G - 1) * DH + (lane % LPR) * EPP));
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor(sum, o, 64);
+        return sum;
+    };
+    float q1 = size_of(0);
+    const int b = paged_find(p, row);
     if (b >= p.B) return;
     const Seq s = paged_seq(p, b);
     if (row < s.row0 || row >= s.row0 + s.n) return;
-    const int have = ((p.causal ? s.past + row - s.row0 : s.len - 1) >> p.lg) + 1;
+    const int have = __builtin_amdgcn_readfirstlane(((p.causal ? s.past + row - s.row0 : s.len - 1) >> p.lg) + 1);
     const int lo = min(a.first, have), hi = max(lo, have - a.last), free = a.budget - lo - (have - hi);      // candidates lo .. hi - 1
-    const uint32_t* key = a.key + (long long)unit * a.slots;
     const int32_t* table = p.table + b * p.table_stride;
-    const In* q_row = reinterpret_cast<const In*>(a.Q) + row * a.ldq + (long long)kvh * p.G * DH;
+    const auto get = [&](int i) { return i >= lo && i < hi ? key[i] : 0u; };
+    uint32_t first[HELD];
+#pragma unroll
+    for (int w = 0; w < HELD; ++w) {
+        if (w * 64 + lane >= have) raw[w] = 0u;            // (what nobody has written)
+        first[w] = w * 64 + lane >= lo && w * 64 + lane < hi ? raw[w] : 0u;
+    }
+    const Keys<uint32_t, HELD, decltype(get)> candidates(have, get, first);
+    // chosen: pages that have to be; keys >= all_from; of the others from between_from on ("open") those whose exact score is above exact_from, and the
+    // first `ties` equal to it
+    uint32_t all_from = 1, between_from = 1;
+    bool many = false;
+    unsigned long long chosen = 0;                         // of up to 64 open ones, by their order
+    int need = 0, open = 0;
+    if (candidates.count(1) > free) {
+        all_from = between_from = 0xFFFFFFFFu;             // (no key is that large)
+        if (free > 0) {
+            // what the scores are exact to
+            for (int h0 = 64 / LPR; h0 < p.G; h0 += 64 / LPR) q1 = fmaxf(q1, size_of(h0));
+            const int sixteens = (have + 15) >> 4;
+            float most = lane < sixteens ? most0 : 0.f;
+            for (int i = 64 + lane; i < sixteens; i += 64) most = fmaxf(most, a.most[(long long)unit * (a.slots >> 4) + i]);
+            q1 = __uint_as_float(max_of_wave(__float_as_uint(q1)));            // (not negative: in the order of their bits)
+            most = __uint_as_float(max_of_wave(__float_as_uint(most)));
+            const float tau = unordered(candidates.kth(free)), err = (2 * DH + 16) * 5.9604645e-8f * q1 * most * 2.02f;
+            between_from = max(ordered(tau - err), 1u);
+            all_from = ordered(tau + err) + 1;
+            const int sure = candidates.count(all_from);
+            open = candidates.count(between_from) - sure;
+            need = free - sure;
+            if (open == need) all_from = between_from;
+            else many = open > 64;
+        }
+    }
+    auto is_open = [&](uint32_t k) { return k >= between_from && k < all_from; };
+    int n = 0, seen = 0;
     int32_t* to = a.list + ((long long)row * p.H_kv + kvh) * a.budget;
-    int n = 0;
     const unsigned long long below = (1ull << lane) - 1;
     auto put_out = [&](bool in, int page) __attribute__((always_inline)) {
         const unsigned long long ins = __builtin_amdgcn_ballot_w64(in);
@@ -265,113 +389,91 @@ __global__ __launch_bounds__(256) void k_select_choose(SelectArgs a) {
         if (in && place < a.budget) to[place] = page;      // (scores that are not numbers can let too many in)
         n = min(n + __popcll(ins), a.budget);
     };
-    auto forced = [&](int from, int end) {
-        for (int i0 = from; i0 < end; i0 += 64) put_out(i0 + lane < end && key[min(i0 + lane, end - 1)] != 0u, i0 + lane);
+    auto forced = [&](int i0, int w, uint32_t k) {         // of the pages that have to be, those that are there
+        const int i = i0 + w * 64 + lane;
+        if (k != 0u || i >= have || (i >= lo && i < hi)) return false;
+        return (i < 64 * HELD ? raw[w] : key[i]) != 0u;
     };
-    forced(0, lo);
-    const auto get = [&](int i) { return key[lo + i]; };
-    const auto candidates = keys_of<uint32_t>(hi - lo, get);
-    // chosen: keys >= all_from; of the others from between_from on ("open") those whose exact score is above exact_from, and the first `ties` equal to it
-    uint32_t all_from = 1, between_from = 1;
-    if (candidates.count(1) <= free) {
-        candidates.each([&](int i0, const uint32_t (&k)[8]) __attribute__((always_inline)) {
+    if (!many) {
+        if (between_from < all_from && open != need) {     // up to 64 open pages, four at a time
+            unsigned long long mine = 0;                   // lane i: the exact score of the i-th
+            int held = 0, at = 0, pages[4] = {0, 0, 0, 0};
+            auto take = [&]() {
+                const In* low[4];
+                double e[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (i0 + i * 64 < hi - lo) put_out(k[i] != 0u, lo + i0 + i * 64 + lane);
-        });
-    } else if (free > 0) {
-        // what the scores are exact to
-        float q1 = 0.f, most = 0.f;
-        for (int h0 = 0; h0 < p.G; h0 += 64 / LPR) {
-            float sum = abs_sum<In>(*reinterpret_cast<const u32x4*>(q_row + (long long)min(h0 + lane / LPR, p.G - 1) * DH + (lane % LPR) * EPP));
+                for (int i = 0; i < 4; ++i) low[i] = reinterpret_cast<const In*>(p.bounds) + ((long long)table[pages[i < held ? i : 0]] * p.H_kv + kvh) * 2 * DH;
+                exact_scores<In, DH>(p.G, q_row, low, e);
 #pragma unroll
-            for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor(sum, o, 64);
-            q1 = fmaxf(q1, sum);
-        }
-        const float* m = a.most + (long long)unit * (a.slots >> 4);
-        for (int i = lane; i < (have + 15) >> 4; i += 64) most = fmaxf(most, m[i]);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            q1 = fmaxf(q1, __shfl_xor(q1, o, 64));
-            most = fmaxf(most, __shfl_xor(most, o, 64));
-        }
-        const float tau = unordered(candidates.kth(free)), err = (2 * DH + 16) * 5.9604645e-8f * q1 * most * 2.02f;
-        between_from = max(ordered(tau - err), 1u);
-        const uint32_t above = ordered(tau + err);
-        all_from = above + 1;
-        const int sure = candidates.count(all_from), open = candidates.count(between_from) - sure, need = free - sure;
-        auto is_open = [&](uint32_t k) { return k >= between_from && k <= above; };
-        if (open == need) all_from = between_from;
-        if (open == need || open <= 64) {
-            unsigned long long chosen = 0;                 // of the open pages, by their order
-            if (open != need) {
-                unsigned long long mine = 0;               // lane i: the exact score of the i-th
-                int i = 0;
-                candidates.each([&](int i0, const uint32_t (&k)[8]) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int w = 0; w < 8; ++w)
-                        for (unsigned long long left = i0 + w * 64 < hi - lo ? __builtin_amdgcn_ballot_w64(is_open(k[w])) : 0ull; left; left &= left - 1, ++i) {
-                            const int page = lo + i0 + w * 64 + __ffsll(left) - 1;
-                            const double e = exact_score<In, DH>(p.G, q_row, reinterpret_cast<const In*>(p.bounds) + ((long long)table[page] * p.H_kv + kvh) * 2 * DH);
-                            if (lane == i) mine = ordered(e);
-                        }
-                });
-                int taken = 0;                             // one place after the other: the largest left, the first of equal ones
-                for (; taken < need; ++taken) {
-                    unsigned long long top = (chosen >> lane) & 1 ? 0ull : mine;
-#pragma unroll
-                    for (int o = 1; o < 64; o <<= 1) {
-                        const unsigned long long other = __shfl_xor(top, o, 64);
-                        top = other > top ? other : top;
-                    }
-                    const unsigned long long at = __builtin_amdgcn_ballot_w64(mine == top && !((chosen >> lane) & 1));
-                    chosen |= at & (~at + 1);
-                }
-            }
-            int seen = 0;
-            candidates.each([&](int i0, const uint32_t (&k)[8]) __attribute__((always_inline)) {
-#pragma unroll
-                for (int w = 0; w < 8; ++w) {
-                    if (i0 + w * 64 >= hi - lo) continue;
-                    const bool o = is_open(k[w]) && k[w] < all_from;
-                    const unsigned long long os = __builtin_amdgcn_ballot_w64(o);
-                    put_out((k[w] != 0u && k[w] >= all_from) || (o && (chosen >> ((seen + __popcll(os & below)) & 63)) & 1), lo + i0 + w * 64 + lane);
-                    seen += __popcll(os);
-                }
-            });
-        } else {
-            // more than 64 within the error of each other (alike pages, queries of zeros): every lane takes the sums of its own pages
-            const auto open_key = [&](int i) {
-                if (!is_open(key[lo + i])) return 0ull;
-                const In* low = reinterpret_cast<const In*>(p.bounds) + ((long long)table[lo + i] * p.H_kv + kvh) * 2 * DH;
-                double best = -INFINITY;
-                for (int h = 0; h < p.G; ++h) {
-                    double sum = 0.0;
-                    for (int c = 0; c < DH; ++c) {
-                        const double x = as_double<In>(q_row[(long long)h * DH + c]);
-                        sum += x * (x < 0.0 ? as_double<In>(low[c]) : as_double<In>(low[DH + c]));
-                    }
-                    best = sum > best ? sum : best;
-                }
-                return ordered(best);
+                for (int i = 0; i < 4; ++i) if (i < held && lane == at + i) mine = ordered(e[i]);
+                at += held;
+                held = 0;
             };
-            const auto opens = keys_of<unsigned long long>(hi - lo, open_key);
-            const unsigned long long exact_from = opens.kth(need);
-            const int ties = need - opens.count(exact_from + 1);
-            int tied = 0;
-            opens.each([&](int i0, const unsigned long long (&e)[8]) __attribute__((always_inline)) {
-                uint32_t k[8];
-                candidates.block(i0, k);
+            candidates.each([&](int i0, const uint32_t (&k)[HELD]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int w = 0; w < 8; ++w) {
-                    if (i0 + w * 64 >= hi - lo) continue;
-                    const unsigned long long ts = __builtin_amdgcn_ballot_w64(e[w] == exact_from);
-                    put_out(k[w] >= all_from || e[w] > exact_from || (e[w] == exact_from && tied + __popcll(ts & below) < ties), lo + i0 + w * 64 + lane);
-                    tied += __popcll(ts);
-                }
+                for (int w = 0; w < HELD; ++w)
+                    for (unsigned long long left = i0 + w * 64 < have ? __builtin_amdgcn_ballot_w64(is_open(k[w])) : 0ull; left; left &= left - 1) {
+                        const int page = i0 + w * 64 + __ffsll(left) - 1;
+                        if (held == 0) pages[0] = page; else if (held == 1) pages[1] = page; else if (held == 2) pages[2] = page; else pages[3] = page;
+                        if (++held == 4) take();
+                    }
             });
+            if (held) take();
+            for (int i = 0; i < need; ++i) {               // one place after the other: the largest left, the first of equal ones
+                unsigned long long top = (chosen >> lane) & 1 ? 0ull : mine;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const unsigned long long other = __shfl_xor(top, o, 64);
+                    top = other > top ? other : top;
+                }
+                const unsigned long long same = __builtin_amdgcn_ballot_w64(mine == top && !((chosen >> lane) & 1));
+                chosen |= same & (~same + 1);
+            }
         }
+        candidates.each([&](int i0, const uint32_t (&k)[HELD]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int w = 0; w < HELD; ++w) {
+                if (i0 + w * 64 >= have) continue;
+                const bool o = is_open(k[w]);
+                const unsigned long long os = __builtin_amdgcn_ballot_w64(o);
+                put_out((k[w] != 0u && k[w] >= all_from) || (o && (chosen >> ((seen + __popcll(os & below)) & 63)) & 1) || forced(i0, w, k[w]), i0 + w * 64 + lane);
+                seen += __popcll(os);
+            }
+        });
+    } else {
+        // more than 64 within the error of each other (alike pages, queries of zeros): every lane takes the sums of its own pages
+        const auto open_key = [&](int i) {
+            if (!is_open(get(i))) return 0ull;
+            const In* low = reinterpret_cast<const In*>(p.bounds) + ((long long)table[i] * p.H_kv + kvh) * 2 * DH;
+            double best = -INFINITY;
+            for (int h = 0; h < p.G; ++h) {
+                double sum = 0.0;
+                for (int c = 0; c < DH; ++c) {
+                    const double x = as_double<In>(q_row[(long long)h * DH + c]);
+                    sum += x * (x < 0.0 ? as_double<In>(low[c]) : as_double<In>(low[DH + c]));
+                }
+                best = sum > best ? sum : best;
+            }
+            return ordered(best);
+        };
+        unsigned long long first_exact[HELD];
+        for (int w = 0; w < HELD; ++w) first_exact[w] = 0;
+        Keys<unsigned long long, HELD, decltype(open_key)> opens(have, open_key, first_exact);
+        opens.block(0, opens.held);
+        const unsigned long long exact_from = opens.kth(need);
+        const int ties = need - opens.count(exact_from + 1);
+        opens.each([&](int i0, const unsigned long long (&e)[HELD]) __attribute__((always_inline)) {
+            uint32_t k[HELD];
+            candidates.block(i0, k);
+#pragma unroll
+            for (int w = 0; w < HELD; ++w) {
+                if (i0 + w * 64 >= have) continue;
+                const unsigned long long ts = __builtin_amdgcn_ballot_w64(e[w] == exact_from);
+                put_out(k[w] >= all_from || e[w] > exact_from || (e[w] == exact_from && seen + __popcll(ts & below) < ties) || forced(i0, w, k[w]), i0 + w * 64 + lane);
+                seen += __popcll(ts);
+            }
+        });
     }
-    forced(hi, have);
     for (int i = n + lane; i < a.budget; i += 64) to[i] = -1;
     if (lane == 0) a.count[(long long)row * p.H_kv + kvh] = n;
 }
@@ -400,16 +502,20 @@ hipError_t launch_select(SelectArgs a, void* ws, hipStream_t st) {
     char* at = reinterpret_cast<char*>(ws) + ADA_PAGED_ZERO_BYTES;
     a.key = reinterpret_cast<uint32_t*>(at);
     a.most = reinterpret_cast<float*>(at + w.most);
-    const int per_group = p.longest == 1 ? 1 : 64;         // rows that share a wave's pages
+    const int per_group = p.longest == 1 ? 1 : 32, pages = p.longest == 1 ? 64 : 128;  // of a workgroup
     for (a.row0 = 0; a.row0 < p.rows; a.row0 += a.rows) {
         a.rows = p.rows - a.row0 < w.rows ? p.rows - a.row0 : w.rows;
         {
             ProfHook ps(ADA_K_ATTN, st);
-            hipLaunchKernelGGL((k_select_scores<In, DH>), dim3((w.slots + 63) / 64, (a.rows + per_group - 1) / per_group, p.H_kv), dim3(256), 0, st, a, per_group);
+            const dim3 grid((w.slots + pages - 1) / pages, (a.rows + per_group - 1) / per_group, p.H_kv);
+            if (p.longest == 1) hipLaunchKernelGGL((k_select_scores<In, DH, 1>), grid, dim3(256), 0, st, a, per_group);
+            else hipLaunchKernelGGL((k_select_scores<In, DH, 2>), grid, dim3(256), 0, st, a, per_group);
         }
         if (hipError_t e = hipGetLastError()) return e;
         ProfHook ps(ADA_K_ATTN, st);
-        hipLaunchKernelGGL((k_select_choose<In, DH>), dim3((unsigned)(((long long)a.rows * p.H_kv + 3) / 4)), dim3(256), 0, st, a);
+        const dim3 grid((unsigned)(((long long)a.rows * p.H_kv + 3) / 4));
+        if (w.slots <= 128) hipLaunchKernelGGL((k_select_choose<In, DH, 2>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_select_choose<In, DH, 8>), grid, dim3(256), 0, st, a);
         if (hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
