@@ -193,12 +193,17 @@ __global__ __launch_bounds__(256) void k_cache_bounds(PagedArgs p, int positions
         float lo[8], hi[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
-#pragma unroll 4
-        for (int k = 0; k < n; k += RPI) {
-            float f[8];
-            Eight<In>::load(keys + (long long)min(k + lane / LPR, n - 1) * p.slot_stride).widen(f);
+        for (int k = 0; k < n; k += 8 * RPI) {             // eight reads under way (behind the last key: that one again)
+            Eight<In> x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { lo[e] = fminf(lo[e], f[e]); hi[e] = fmaxf(hi[e], f[e]); }
+            for (int i = 0; i < 8; ++i) x[i] = Eight<In>::load(keys + (long long)min(k + i * RPI + lane / LPR, n - 1) * p.slot_stride);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float f[8];
+                x[i].widen(f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { lo[e] = fminf(lo[e], f[e]); hi[e] = fmaxf(hi[e], f[e]); }
+            }
         }
 #pragma unroll
         for (int o = LPR; o < 64; o <<= 1)

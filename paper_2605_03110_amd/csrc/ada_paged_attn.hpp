@@ -586,7 +586,9 @@ struct AttendWs { size_t tiles, prefix, tile, part_o, part_ml, bytes; };
 // Chunks whose rows fill a good part of a 128-row tile go to ada_paged_tile.hpp's kernel.
 inline bool takes_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G >= 48; }
 
-inline int rows_pieces() { return 4 * ada_hook_cus() < ADA_PAGED_ZERO_BYTES / 4 ? 4 * ada_hook_cus() : ADA_PAGED_ZERO_BYTES / 4; }
+// Two workgroups per CU: 64 single tokens at 100 to 8191 keys, 32 x 128 over 8, us a call with 1, 2, 3, 4 of them: 101, 102, 118, 111 (registers hold two at
+// once); 1024 tokens with 16 listed pages of 64: 597, 422, 477, 422.
+inline int rows_pieces() { return 2 * ada_hook_cus() < ADA_PAGED_ZERO_BYTES / 4 ? 2 * ada_hook_cus() : ADA_PAGED_ZERO_BYTES / 4; }
 inline int tile_pieces(int d_h) { const int n = (d_h > 128 ? 1 : 2) * ada_hook_cus(); return n < rows_pieces() ? n : rows_pieces(); }
 
 inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {

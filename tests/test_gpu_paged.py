@@ -521,3 +521,31 @@ def test_no_rows(pa):
     out = torch.full((1, 128), 7.0, dtype=torch.bfloat16, device="cuda")
     assert pa.ada_attention_paged(cache, chunk, some, out=out)["status"].item() == OK
     assert bool((out == 7.0).all())
+
+
+def test_append_of_a_large_chunk(pa):
+    """17000 tokens at once and in pieces of 5000 that end inside pages: the same to the bit."""
+    H, H_kv, d_h, page, n = 32, 8, 128, 64, 17000
+    rows, heads = torch.arange(n, device="cuda"), H + 2 * H_kv
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    qkv = torch.randn(n, heads * d_h, generator=gen, device="cuda").bfloat16()
+    rope = ref.rope_table(n, d_h).cuda()
+    w = (1 + 0.2 * torch.randn(d_h, generator=gen, device="cuda")).bfloat16()
+    pages = -(-n // page)
+    table = torch.randperm(pages, generator=gen, device="cuda").int()[None].contiguous()
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    got = []
+    for step in (n, 5000):
+        K = torch.zeros(pages, H_kv, page, d_h, dtype=torch.bfloat16, device="cuda")
+        cache = pa.PagedCache(K, torch.zeros_like(K), torch.zeros(pages, H_kv, 2, d_h, dtype=torch.bfloat16, device="cuda"))
+        qs = []
+        for lo in range(0, n, step):
+            hi = min(lo + step, n)
+            q, k, v = qkv[lo:hi].split((H * d_h, H_kv * d_h, H_kv * d_h), dim=1)
+            res = pa.ada_cache_append(cache, pa.Chunk(table, ints(0, hi - lo), ints(lo), rows=hi - lo), q, k, v, rope=rope, q_norm=w, k_norm=w)
+            assert res["status"].item() == OK
+            qs.append(res["q"])
+        got.append((torch.cat(qs), cache.K, cache.V, cache.bounds))
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+    assert torch.equal(got[0][2][table[0, rows // page].long(), :, rows % page], qkv[:, -H_kv * d_h:].view(n, H_kv, d_h))
