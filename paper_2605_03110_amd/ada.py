@@ -6,7 +6,6 @@ result to the host and raises on a device-reported status.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 import subprocess
@@ -733,7 +732,7 @@ class PagedCache:
         if bounds is not None and (tuple(bounds.shape) != (pages, H_kv, 2, d_h) or bounds.dtype != K.dtype or bounds.device != K.device
                                    or not bounds.is_contiguous()):
             raise ValueError("bounds must be a contiguous [pages, H_kv, 2, d_h] tensor like K")
-        self.K, self.V, self.bounds = K, V, bounds
+        self.K, self.V, self.bounds, self.dtype, self.device = K, V, bounds, K.dtype, K.device
         self.pages, self.H_kv, self.page, self.d_h = pages, H_kv, page, d_h
         # (a dimension of one element steps nowhere: its stride is torch's to choose)
         self.desc = AdaPagedCache(_ptr(K), _ptr(V), _ptr(bounds), pages, page, H_kv, d_h, _dtype_code(K),
@@ -754,7 +753,7 @@ class Chunk:
             raise ValueError("table must be [B, max_pages] with contiguous rows")
         if start.dim() != 1 or past.dim() != 1 or start.numel() != B + 1 or not start.is_contiguous() or not past.is_contiguous():
             raise ValueError("start must be [B + 1] and past [B], both contiguous")
-        self.table, self.start, self.past, self.B, self.rows = table, start, past, B, int(rows)
+        self.table, self.start, self.past, self.B, self.rows, self.device = table, start, past, B, int(rows), table.device
         self.desc = AdaPagedChunk(B, self.rows, self.rows if longest is None else int(longest), table.shape[1], _ptr(table),
                                   table.stride(0) if B > 1 else table.shape[1], _ptr(start), _ptr(past))
         self.ref = ctypes.byref(self.desc)
@@ -769,38 +768,44 @@ def paged_workspace(cache: PagedCache, chunk: Chunk, H: int) -> torch.Tensor:
     n = ada_paged_workspace_bytes(cache, chunk, H)
     if n == 0:
         raise ValueError("sizes that no paged attention takes")
-    ws = torch.empty(n, dtype=torch.uint8, device=cache.K.device)
+    ws = torch.empty(n, dtype=torch.uint8, device=cache.device)
     ws[:PAGED_ZERO_BYTES].zero_()
     return ws
 
 
-def _paged_rows(cache: PagedCache, chunk: Chunk, X: torch.Tensor, name: str, heads: Optional[int] = None) -> int:
-    """The heads of rows x (heads * d_h)."""
-    if X.dim() != 2 or X.dtype != cache.K.dtype or X.device != cache.K.device or (X.shape[1] > 1 and X.stride(1) != 1):
-        raise ValueError("%s must be a rows x (heads * d_h) tensor of the cache's dtype and device with unit column stride" % name)
-    n = X.shape[1] // cache.d_h
-    if X.shape[0] < chunk.rows or n * cache.d_h != X.shape[1] or (heads is not None and n != heads):
+def _paged_rows(cache: PagedCache, chunk: Chunk, X: torch.Tensor, name: str, heads: Optional[int] = None):
+    """(heads, leading dimension) of rows x (heads * d_h).  (Single tokens take 5 us on the GPU: tensors are asked as little as can be.)"""
+    if X.dtype is not cache.dtype or X.dim() != 2 or X.device != cache.device:
+        raise ValueError("%s must be a rows x (heads * d_h) tensor of the cache's dtype and device" % name)
+    rows, width = X.shape
+    ld, step = X.stride()
+    if step != 1 and width > 1:
+        raise ValueError("%s must have unit column stride" % name)
+    n = width // cache.d_h
+    if rows < chunk.rows or n * cache.d_h != width or (heads is not None and n != heads):
         raise ValueError("%s must have %d rows (or more) and %s heads of %d" % (name, chunk.rows, "some" if heads is None else heads, cache.d_h))
-    return n
+    return n, ld if rows > 1 else width                    # (one row steps nowhere)
 
 
 def _paged_status(cache: PagedCache, status: Optional[torch.Tensor]) -> torch.Tensor:
     if status is None:
-        return torch.zeros(1, dtype=torch.int32, device=cache.K.device)
-    if status.dtype != torch.int32 or status.device != cache.K.device or status.numel() < 1:
+        return torch.zeros(1, dtype=torch.int32, device=cache.device)
+    if status.dtype is not torch.int32 or status.device != cache.device or status.numel() < 1:
         raise ValueError("status must be an int32 tensor on the cache's device")
     return status
 
 
-def _ld(X: torch.Tensor) -> int:
-    return X.stride(0) if X.shape[0] > 1 else X.shape[1]       # (one row steps nowhere)
-
-
-def _on(cache: PagedCache, chunk: Chunk):
-    """The cache's device as the current one, for calls made beside another."""
-    if chunk.table.device != cache.K.device:
+def _paged_call(cache: PagedCache, chunk: Chunk, f, name: str) -> None:
+    """f() with the cache's device as the current one."""
+    if chunk.device != cache.device:
         raise ValueError("cache and chunk must share their device")
-    return torch.cuda.device(cache.K.device) if cache.K.device.index != torch._C._cuda_getDevice() else contextlib.nullcontext()
+    if cache.device.index == torch._C._cuda_getDevice():
+        rc = f()
+    else:
+        with torch.cuda.device(cache.device):
+            rc = f()
+    if rc != OK:
+        raise AdaError(rc, name)
 
 
 def ada_cache_append(cache: PagedCache, chunk: Chunk, Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, *,
@@ -810,48 +815,48 @@ def ada_cache_append(cache: PagedCache, chunk: Chunk, Q: Optional[torch.Tensor],
     """Norm per head, rotation, and the new tokens' keys and values into the cache (its bounds widened where it has them).  Q, K, V: rows x
     (heads * d_h), views of one projection's output if need be; Q may be None.  rope: [positions, rot / 2, 2] float32 cosines and sines; q_norm,
     k_norm: [d_h] weights or None.  Returns q (`out` if given; may be Q) and status, an int32 word that errors raise."""
-    H = None if Q is None else _paged_rows(cache, chunk, Q, "Q")
-    _paged_rows(cache, chunk, K, "K", cache.H_kv)
-    _paged_rows(cache, chunk, V, "V", cache.H_kv)
+    H, ldq = (None, 0) if Q is None else _paged_rows(cache, chunk, Q, "Q")
+    ldk, ldv, ldo = _paged_rows(cache, chunk, K, "K", cache.H_kv)[1], _paged_rows(cache, chunk, V, "V", cache.H_kv)[1], 0
     for w, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-        if w is not None and (tuple(w.shape) != (cache.d_h,) or w.dtype != K.dtype or w.device != K.device or not w.is_contiguous()):
+        if w is not None and (w.shape != (cache.d_h,) or w.dtype is not cache.dtype or w.device != cache.device or not w.is_contiguous()):
             raise ValueError("%s must be a contiguous [d_h] tensor like K" % name)
-    if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2 or rope.dtype != torch.float32 or rope.device != K.device or not rope.is_contiguous()):
-        raise ValueError("rope must be a contiguous float32 [positions, rot / 2, 2] device tensor")
+    positions = rot = 0
+    if rope is not None:
+        if rope.dim() != 3 or rope.shape[2] != 2 or rope.dtype is not torch.float32 or rope.device != cache.device or not rope.is_contiguous():
+            raise ValueError("rope must be a contiguous float32 [positions, rot / 2, 2] device tensor")
+        positions, half, _ = rope.shape
+        rot = 2 * half
     status = _paged_status(cache, status)
     if Q is None:
         out = None
     elif out is None:
-        out = torch.empty((Q.shape[0], Q.shape[1]), dtype=Q.dtype, device=Q.device)
+        out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        ldo = Q.shape[1]
     else:
-        _paged_rows(cache, chunk, out, "out", H)
-    with _on(cache, chunk):
-        rc = lib().ada_cache_append(cache.ref, chunk.ref, _ptr(Q), 0 if Q is None else _ld(Q), _ptr(K), _ld(K), _ptr(V), _ld(V),
-                                    cache.H_kv if H is None else H, _ptr(q_norm), _ptr(k_norm), float(eps), _ptr(rope),
-                                    0 if rope is None else 2 * rope.shape[1], 0 if rope is None else rope.shape[0], _ptr(out),
-                                    0 if out is None else _ld(out), _ptr(status), _stream(stream), int(flags))
-    if rc != OK:
-        raise AdaError(rc, "ada_cache_append")
+        ldo = _paged_rows(cache, chunk, out, "out", H)[1]
+    _paged_call(cache, chunk, lambda: lib().ada_cache_append(
+        cache.ref, chunk.ref, _ptr(Q), ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, cache.H_kv if H is None else H, _ptr(q_norm), _ptr(k_norm), eps,
+        _ptr(rope), rot, positions, _ptr(out), ldo, status.data_ptr(), _stream(stream), flags), "ada_cache_append")
     return dict(q=out, status=status, _keep=(cache, chunk, Q, K, V, rope, q_norm, k_norm))
 
 
 def _paged_attention(cache, chunk, Q, lists, ws, out, status, stream, flags, name):
-    H = _paged_rows(cache, chunk, Q, "Q")
+    H, ldq = _paged_rows(cache, chunk, Q, "Q")
     status = _paged_status(cache, status)
     ws = paged_workspace(cache, chunk, H) if ws is None else ws
     if out is None:
-        out = torch.empty((Q.shape[0], Q.shape[1]), dtype=Q.dtype, device=Q.device)
+        out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        ldo = Q.shape[1]
     else:
-        _paged_rows(cache, chunk, out, "out", H)
-    with _on(cache, chunk):
-        if lists is None:
-            rc = lib().ada_attention_paged(cache.ref, chunk.ref, _ptr(Q), H, _ld(Q), _ptr(out), _ld(out), _ptr(status), _ptr(ws), ws.numel(),
-                                           _stream(stream), int(flags))
-        else:
-            rc = lib().ada_attention_pages(cache.ref, chunk.ref, _ptr(Q), H, _ld(Q), _ptr(lists[0]), _ptr(lists[1]), lists[0].shape[2], _ptr(out),
-                                           _ld(out), _ptr(status), _ptr(ws), ws.numel(), _stream(stream), int(flags))
-    if rc != OK:
-        raise AdaError(rc, name)
+        ldo = _paged_rows(cache, chunk, out, "out", H)[1]
+    if lists is None:
+        _paged_call(cache, chunk, lambda: lib().ada_attention_paged(
+            cache.ref, chunk.ref, Q.data_ptr(), H, ldq, out.data_ptr(), ldo, status.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream), flags), name)
+    else:
+        pages, counts = lists
+        _paged_call(cache, chunk, lambda: lib().ada_attention_pages(
+            cache.ref, chunk.ref, Q.data_ptr(), H, ldq, pages.data_ptr(), counts.data_ptr(), pages.shape[2], out.data_ptr(), ldo, status.data_ptr(),
+            ws.data_ptr(), ws.numel(), _stream(stream), flags), name)
     return dict(out=out, status=status, _keep=(cache, chunk, Q, lists, ws))
 
 
@@ -864,10 +869,11 @@ def ada_attention_paged(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, *, ws:
 
 
 def _check_lists(cache, chunk, pages, counts):
-    if pages.dtype != torch.int32 or pages.dim() != 3 or pages.shape[0] < chunk.rows or pages.shape[1] != cache.H_kv or not pages.is_contiguous() \
-            or pages.device != cache.K.device:
+    shape = pages.shape
+    if pages.dtype is not torch.int32 or len(shape) != 3 or shape[0] < chunk.rows or shape[1] != cache.H_kv or not pages.is_contiguous() \
+            or pages.device != cache.device:
         raise ValueError("pages must be a contiguous [rows, H_kv, budget] int32 tensor on the cache's device")
-    if counts.dtype != torch.int32 or tuple(counts.shape) != tuple(pages.shape[:2]) or not counts.is_contiguous() or counts.device != pages.device:
+    if counts.dtype is not torch.int32 or counts.shape != shape[:2] or not counts.is_contiguous() or counts.device != cache.device:
         raise ValueError("counts must be a contiguous [rows, H_kv] int32 tensor beside pages")
 
 
@@ -877,23 +883,22 @@ def ada_select_pages(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, budget: i
     """For every row and head of the cache the `budget` pages of its sequence that its queries may weigh most, by the pages' bounds; the
     `first` and `last` pages it sees are always among them.  Returns pages [rows, H_kv, budget] int32 (ascending, -1 behind the last), counts
     [rows, H_kv] int32 (`out`'s, if given) and status."""
-    H = _paged_rows(cache, chunk, Q, "Q")
+    H, ldq = _paged_rows(cache, chunk, Q, "Q")
     if cache.bounds is None:
         raise ValueError("the cache has no bounds to score pages by")
     status = _paged_status(cache, status)
     if out is None:
-        out = dict(pages=torch.empty((chunk.rows, cache.H_kv, int(budget)), dtype=torch.int32, device=Q.device),
-                   counts=torch.empty((chunk.rows, cache.H_kv), dtype=torch.int32, device=Q.device))
-    _check_lists(cache, chunk, out["pages"], out["counts"])
-    if out["pages"].shape[2] != int(budget):
+        out = dict(pages=torch.empty((chunk.rows, cache.H_kv, int(budget)), dtype=torch.int32, device=cache.device),
+                   counts=torch.empty((chunk.rows, cache.H_kv), dtype=torch.int32, device=cache.device))
+    pages, counts = out["pages"], out["counts"]
+    _check_lists(cache, chunk, pages, counts)
+    if pages.shape[2] != budget:
         raise ValueError("pages must have `budget` entries per row and head")
     ws = paged_workspace(cache, chunk, H) if ws is None else ws
-    with _on(cache, chunk):
-        rc = lib().ada_select_pages(cache.ref, chunk.ref, _ptr(Q), H, _ld(Q), int(budget), int(first), int(last), _ptr(out["pages"]),
-                                    _ptr(out["counts"]), _ptr(status), _ptr(ws), ws.numel(), _stream(stream), int(flags))
-    if rc != OK:
-        raise AdaError(rc, "ada_select_pages")
-    return dict(pages=out["pages"], counts=out["counts"], status=status, _keep=(cache, chunk, Q, ws))
+    _paged_call(cache, chunk, lambda: lib().ada_select_pages(
+        cache.ref, chunk.ref, Q.data_ptr(), H, ldq, budget, first, last, pages.data_ptr(), counts.data_ptr(), status.data_ptr(), ws.data_ptr(), ws.numel(),
+        _stream(stream), flags), "ada_select_pages")
+    return dict(pages=pages, counts=counts, status=status, _keep=(cache, chunk, Q, ws))
 
 
 def ada_attention_pages(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, pages: torch.Tensor, counts: torch.Tensor, *,
