@@ -37,8 +37,8 @@ enum { CHUNKS,                                             // sequences of many 
        TOKENS,                                             // a tile per sequence: every wave sums up the lengths itself
        LISTED };                                           // listed pages: tiles of one row, all alike
 
-// One workgroup.
-__global__ __launch_bounds__(1024) void k_paged_plan(PagedArgs p, int tile_rows, int unit, long long* prefix, int2* tile, int* tiles) {
+// One workgroup.  `room`: tiles that prefix and tile hold; more can only be where sequences overlap (a start that descends): they are left out.
+__global__ __launch_bounds__(1024) void k_paged_plan(PagedArgs p, int tile_rows, int unit, int room, long long* prefix, int2* tile, int* tiles) {
     __shared__ int base[ADA_MAX_BATCH + 1];
     __shared__ long long sums[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -58,9 +58,10 @@ __global__ __launch_bounds__(1024) void k_paged_plan(PagedArgs p, int tile_rows,
     int carry = 0;
     for (int b0 = 0; b0 < p.B; b0 += 1024) {
         const int b = b0 + tid;
-        const int mine = b < p.B ? (int)(((long long)paged_seq(p, b).n * p.G + tile_rows - 1) / tile_rows) : 0;
-        const int upto = carry + (int)scan(mine);
-        if (b < p.B) base[b + 1] = upto;
+        const long long mine = b < p.B ? ((long long)paged_seq(p, b).n * p.G + tile_rows - 1) / tile_rows : 0;
+        const long long upto = carry + scan(mine);
+        if (upto > room) raise(p, ADA_ERR_SHAPE);
+        if (b < p.B) base[b + 1] = (int)min(upto, (long long)room);
         __syncthreads();
         carry = base[min(b0 + 1024, p.B)];
     }
@@ -581,7 +582,7 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
 #include "ada_paged_tile.hpp"
 
 // ------------------------------------------------------------------------------------------------ host
-struct AttendWs { size_t tiles, prefix, tile, part_o, part_ml, bytes; };
+struct AttendWs { size_t tiles, prefix, tile, part_o, part_ml, bytes; int room; };
 
 // Chunks whose rows fill a good part of a 128-row tile go to ada_paged_tile.hpp's kernel.
 inline bool takes_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G >= 48; }
@@ -597,6 +598,7 @@ inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
     const size_t parts = 2 * (rows > tile_rows ? rows : tile_rows);           // rows of cut tiles (listed pages always take 16-row ones)
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     AttendWs w;
+    w.room = (int)tiles;
     w.tiles = ADA_PAGED_ZERO_BYTES;                        // behind what is zero between calls
     w.prefix = w.tiles + 256;
     w.tile = w.prefix + up((tiles + 1) * 8);
@@ -647,7 +649,7 @@ hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
     if (!chunks && (long long)a.p.longest * a.p.G <= TILE_ROWS) return launch_rows<In, DH, TOKENS>(a, st);
     {
         ProfHook ps(ADA_K_ATTN, st);
-        hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, chunks ? TileGeom<DH>::ROWS : TILE_ROWS, chunks ? TileGeom<DH>::KEYS : UNIT, prefix, tile, tiles);
+        hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, chunks ? TileGeom<DH>::ROWS : TILE_ROWS, chunks ? TileGeom<DH>::KEYS : UNIT, w.room, prefix, tile, tiles);
     }
     if (hipError_t e = hipGetLastError()) return e;
     if constexpr (dtype == ADA_BF16)

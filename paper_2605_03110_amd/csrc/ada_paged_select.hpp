@@ -176,10 +176,10 @@ __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a, int per_gro
     constexpr int EPP = 16 / (int)sizeof(In), KF = DH / (4 * EPP);
     const PagedArgs& p = a.p;
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, kvh = blockIdx.z;
-    const int j0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 16 * SETS;
+    const int j0 = (blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 16 * SETS;
     const int per = 1 << a.lg_heads, tokens = 16 >> a.lg_heads;                // columns: a token's heads side by side
-    const int end = min((int)(blockIdx.y + 1) * per_group, a.rows) + a.row0;
-    for (int row = blockIdx.y * per_group + a.row0; row < end;) {
+    const int end = min((int)(blockIdx.x + 1) * per_group, a.rows) + a.row0;
+    for (int row = blockIdx.x * per_group + a.row0; row < end;) {
         const int b = paged_find(p, row);
         if (b >= p.B) return;                                                  // rows behind the last sequence
         const Seq s = paged_seq(p, b);
@@ -507,7 +507,7 @@ hipError_t launch_select(SelectArgs a, void* ws, hipStream_t st) {
         a.rows = p.rows - a.row0 < w.rows ? p.rows - a.row0 : w.rows;
         {
             ProfHook ps(ADA_K_ATTN, st);
-            const dim3 grid((w.slots + pages - 1) / pages, (a.rows + per_group - 1) / per_group, p.H_kv);
+            const dim3 grid((a.rows + per_group - 1) / per_group, (w.slots + pages - 1) / pages, p.H_kv);
             if (p.longest == 1) hipLaunchKernelGGL((k_select_scores<In, DH, 1>), grid, dim3(256), 0, st, a, per_group);
             else hipLaunchKernelGGL((k_select_scores<In, DH, 2>), grid, dim3(256), 0, st, a, per_group);
         }

@@ -40,6 +40,11 @@ ATTEND = {
     "chunk_f32_128": lambda: ref.Case("f32", 2, 1, 128, 16, [40, 3], [0, 130]),
     "mixed": lambda: ref.Case("bf16", 8, 2, 128, 16, [1, 0, 33, 300, 1, 0, 2], [40, 9, 0, 17, 513, 0, 64], pad_rows=5),
     "large_scores": lambda: ref.Case("bf16", 4, 2, 128, 32, [130, 1], [70, 400], scale=8.0),
+    "many_tokens": lambda: ref.Case("bf16", 4, 1, 64, 16, [1] * 150, [(37 * b) % 331 for b in range(150)]),
+    "many_chunks": lambda: ref.Case("bf16", 4, 2, 64, 32, [(b * 7) % 23 for b in range(130)], [(37 * b) % 200 for b in range(130)]),
+    "many_chunks_f32": lambda: ref.Case("f32", 4, 2, 64, 16, [(b * 7) % 9 for b in range(70)], [(37 * b) % 90 for b in range(70)]),
+    "long_token": lambda: ref.Case("bf16", 2, 1, 128, 256, [1], [70000]),
+    "long_chunk": lambda: ref.Case("bf16", 16, 1, 64, 16, [9], [20000]),
     "values_off_zero": lambda: ref.Case("bf16", 4, 2, 64, 16, [64, 1], [0, 900], value_shift=3.0),
 }
 
@@ -121,6 +126,25 @@ def test_sequences_that_do_not_fit_are_left_out(pa):
         room = ref.tolerance(c, want, weight, err, step_of(c))
         keep = [0, 1, 2] + ([] if what == "behind" else [4, 5])
         assert bool(((out.double().cpu() - want).abs() <= room)[keep].all())
+
+
+@pytest.mark.parametrize("longest", (1, 8, 40))
+def test_sequences_that_overlap_stay_in_bounds(pa, longest):
+    """Starts that go back and forth: more tiles than rows make.  Whatever is written, it is written inside, and the call says so."""
+    c = ref.Case("bf16", 4, 2, 64, 16, [longest] * 3, [20, 7, 30])
+    cache, _ = c.on_gpu(pa)
+    B = 600
+    start = torch.tensor([0, longest] * (B // 2) + [0], dtype=torch.int32, device="cuda")
+    table = c.table[:1].repeat(B, 1).cuda()
+    chunk = pa.Chunk(table, start, torch.full((B,), 3, dtype=torch.int32, device="cuda"), rows=longest, longest=longest)
+    ws = pa.paged_workspace(cache, chunk, c.H)
+    guard = torch.full((ws.numel() + 4096,), 77, dtype=torch.uint8, device="cuda")
+    guard[:ws.numel()] = ws
+    out = torch.full((longest + 1, c.H * 64), 7.0, dtype=c.dtype, device="cuda")
+    res = pa.ada_attention_paged(cache, chunk, c.Q[:longest].cuda(), ws=guard[:ws.numel()], out=out, flags=pa.FLAG_ATTN_CAUSAL)
+    assert res["status"].item() == SHAPE
+    assert bool((out[longest] == 7.0).all()) and bool((guard[ws.numel():] == 77).all())
+    assert bool((guard[:pa.PAGED_ZERO_BYTES] == 0).all())
 
 
 def test_status_is_raised_and_never_cleared(pa):
@@ -251,6 +275,7 @@ SELECT = {
     "all_of_them": (lambda: ref.Case("bf16", 2, 1, 64, 16, [20], [100]), 64, 1, 1),
     "one_page": (lambda: ref.Case("bf16", 4, 2, 128, 64, [3, 1], [500, 900]), 1, 0, 1),
     "only_forced": (lambda: ref.Case("bf16", 4, 2, 64, 16, [6], [400]), 4, 2, 2),
+    "long_chunk": (lambda: ref.Case("bf16", 6, 2, 64, 16, [70, 33], [3000, 100]), 12, 1, 1),
     "many_pages": (lambda: ref.Case("bf16", 2, 1, 64, 16, [1], [20000]), 40, 1, 1),
 }
 
@@ -283,8 +308,8 @@ def test_select(pa, name, causal):
 
 def test_select_ties_and_near_ties(pa):
     """Pages alike to the bit, scores that differ in fp32's last places only, and queries of zeros: as in float64, ties to the smaller page."""
-    for kind in ("alike", "near", "zero", "f32"):
-        c = ref.Case("f32" if kind == "f32" else "bf16", 4, 2, 128, 16, [3, 1], [700, 500])
+    for kind, past in [(k, 700) for k in ("alike", "near", "zero", "f32")] + [("alike", 1700), ("zero", 1700), ("near", 10000), ("zero", 10000)]:
+        c = ref.Case("f32" if kind == "f32" else "bf16", 4, 2, 128, 16, [3, 1] if past < 9000 else [1], [past, 500] if past < 9000 else [past])
         g = torch.Generator().manual_seed(5)
         if kind == "alike":
             c.bounds[:] = c.bounds[int(c.table[0, 0])].clone()
