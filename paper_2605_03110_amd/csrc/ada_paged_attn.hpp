@@ -341,73 +341,90 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
         const long long lrow = MODE == LISTED ? (long long)t.row * p.H_kv + t.kvh : 0;
         const int32_t* list = MODE == LISTED ? a.list + lrow * a.budget : nullptr;
         const int n_list = MODE == LISTED ? min(max(a.count[lrow], 0), a.budget) : 0;
-        const long long head_at = t.kvh * p.head_stride;
+        const int n_pages = MODE == LISTED ? n_list : ((t.s.len - 1) >> p.lg) + 1;
 
-        // 16 keys: their first position (NOWHERE: nothing to see) and place in the cache
-        auto resolve = [&](int v, int& pos, long long& at) {
-            pos = NOWHERE;
-            at = 0;
-            int lp = v >> p.lg, ps = v;
-            if (MODE == LISTED) {
-                if (lp >= n_list) return;
-                const int i = lp, before = i > 0 ? list[i - 1] : -1;
-                lp = list[i];
-                if (lp <= before || lp > (t.s.len - 1) >> p.lg) { raise(p, ADA_ERR_INDEX); return; }
-                ps = (lp << p.lg) + (v & ((1 << p.lg) - 1));
+        // Pages, 64 at a time, a lane each: number in the sequence (listed ones are in any place) and in the pool, -1 where there is none.  The even sixty-fours and
+        // the odd ones; the next come in while this one's keys are taken, so that no unit waits for a number.
+        struct Window { int named, page; };
+        auto window = [&](int w) {
+            const int i = w * 64 + lane;
+            Window r = {i, -1};
+            bool ok = i < n_pages;
+            if (MODE == LISTED && ok) {
+                const int before = i > 0 ? list[i - 1] : -1;
+                r.named = list[i];
+                ok = r.named > before && r.named <= (t.s.len - 1) >> p.lg;
+                if (!ok) raise(p, ADA_ERR_INDEX);
             }
-            if (ps >= t.s.len) return;
-            const int page = p.table[t.b * p.table_stride + lp];
-            if (page < 0 || page >= p.pages) { raise(p, ADA_ERR_INDEX); return; }
-            pos = ps;
-            at = page * p.page_stride + (ps & ((1 << p.lg) - 1)) * p.slot_stride + head_at;
+            if (ok) {
+                r.page = p.table[t.b * p.table_stride + r.named];
+                if (r.page < 0 || r.page >= p.pages) {
+                    raise(p, ADA_ERR_INDEX);
+                    r.page = -1;
+                }
+            }
+            return r;
         };
+        const int lg_span = p.lg - 1;                      // units of a window
+        Window even, odd;
+        {
+            const int w = k0 >> lg_span;
+            const Window w0 = window(w), w1 = window(w + 1);
+            even = w & 1 ? w1 : w0;
+            odd = w & 1 ? w0 : w1;
+        }
+        // the wave's two groups of 16 keys: first position (NOWHERE: nothing to see), the last row that is there, where they lie
         u32x4 kf[2][KF], vf[VF];
-        int pos[2];
-        long long at[2];
+        int pos[2], rows[2];
+        const char *kat[2], *vat[2];
+        const uint32_t step = (uint32_t)p.slot_stride * (uint32_t)sizeof(In);          // bytes from key to key: 15 of them fit into 32 bits
         auto where = [&](int u) {                          // false: none of the wave's 32 keys of unit u is there
-            const int v = u * UNIT + wave * WAVE_KEYS;
-            resolve(v, pos[0], at[0]);
-            resolve(v + 16, pos[1], at[1]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) pos[i] = __builtin_amdgcn_readfirstlane(pos[i]);
-            return pos[0] != NOWHERE || pos[1] != NOWHERE;
+            for (int i = 0; i < 2; ++i) {
+                const int v = u * UNIT + wave * WAVE_KEYS + 16 * i, n = v >> p.lg, in = v & ((1 << p.lg) - 1);
+                const bool second = (n >> 6) & 1;
+                const int page = __builtin_amdgcn_readlane(second ? odd.page : even.page, n & 63);
+                const int named = MODE == LISTED ? __builtin_amdgcn_readlane(second ? odd.named : even.named, n & 63) : n;
+                pos[i] = n < n_pages && page >= 0 ? (named << p.lg) + in : NOWHERE;
+                if (pos[i] >= t.s.len) pos[i] = NOWHERE;
+                rows[i] = t.s.len - 1 - pos[i];
+                const long long at = (page * p.page_stride + in * p.slot_stride + t.kvh * p.head_stride) * (long long)sizeof(In);
+                kat[i] = reinterpret_cast<const char*>(p.K) + at;
+                vat[i] = reinterpret_cast<const char*>(p.V) + at;
+            }
+            if (pos[0] == NOWHERE && pos[1] == NOWHERE) return false;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (pos[i] == NOWHERE) { rows[i] = rows[1 - i]; kat[i] = kat[1 - i]; vat[i] = vat[1 - i]; }     // (read, and seen by nobody)
+            return true;
         };
         // rows behind the sequence's end are not read: the last one stands in (its weight is 0)
-        auto row_of = [&](int i, int r, int& base) {
-            base = pos[i] != NOWHERE ? i : 1 - i;
-            return min(r, t.s.len - 1 - pos[base]);
-        };
+        const uint32_t koff = l16 * step + g * 16;
         auto fetch_k = [&]() {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                int base;
-                const int r = row_of(i, l16, base);
-                const In* k = reinterpret_cast<const In*>(p.K) + at[base] + r * p.slot_stride + g * R::EPP;
+                const uint32_t off = rows[i] >= 15 ? koff : min(l16, rows[i]) * step + g * 16;
 #pragma unroll
-                for (int c = 0; c < KF; ++c) kf[i][c] = *reinterpret_cast<const u32x4*>(k + c * 4 * R::EPP);
+                for (int c = 0; c < KF; ++c) kf[i][c] = *reinterpret_cast<const u32x4*>(kat[i] + off + c * 64);
             }
         };
         auto fetch_v = [&]() {
             if constexpr (sizeof(In) == 2) {               // rows by pieces, as LDS takes them
-                constexpr int PPR = DH / 8;
+                constexpr int PPR = DH / 8, RPI = 64 / PPR;
 #pragma unroll
                 for (int u = 0; u < VF; ++u) {
-                    const int i = u * 64 + lane, r32 = i / PPR;
-                    int b0, b1;
-                    const int r0 = row_of(0, r32 & 15, b0), r1 = row_of(1, r32 & 15, b1);
-                    const long long off = r32 < 16 ? at[b0] + r0 * p.slot_stride : at[b1] + r1 * p.slot_stride;
-                    vf[u] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const In*>(p.V) + off + (i % PPR) * 8);
+                    const int i = u * RPI / 16, r = u * RPI % 16;
+                    const uint32_t off = (rows[i] >= 15 ? (lane / PPR) * step + r * step : min(r + lane / PPR, rows[i]) * step) + (lane % PPR) * 16;
+                    vf[u] = *reinterpret_cast<const u32x4*>(vat[i] + off);
                 }
             } else {                                       // columns l16 DH / 16 .. of keys 4 g + e
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        int base;
-                        const int r = row_of(i, 4 * g + e, base);
-                        const In* v = reinterpret_cast<const In*>(p.V) + at[base] + r * p.slot_stride + l16 * (DH / 16);
+                        const uint32_t off = (rows[i] >= 15 ? 4 * g * step + e * step : min(4 * g + e, rows[i]) * step) + l16 * (DH / 4);
 #pragma unroll
-                        for (int c = 0; c < DH / 64; ++c) vf[(i * 4 + e) * (DH / 64) + c] = *reinterpret_cast<const u32x4*>(v + 4 * c);
+                        for (int c = 0; c < DH / 64; ++c) vf[(i * 4 + e) * (DH / 64) + c] = *reinterpret_cast<const u32x4*>(vat[i] + off + 16 * c);
                     }
             }
         };
@@ -419,6 +436,10 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
         bool have = where(k0);
         if (have) { fetch_k(); fetch_v(); }
         for (int u = k0; u < k1; ++u) {
+            if ((u & ((1 << lg_span) - 1)) == 0 && u > k0 && u + (1 << lg_span) < k1) {      // (the window before this one is done with)
+                const Window next = window((u >> lg_span) + 1);
+                if ((u >> lg_span) & 1) even = next; else odd = next;
+            }
             if (!have) {
                 if (u + 1 < k1 && (have = where(u + 1))) { fetch_k(); fetch_v(); }
                 continue;
