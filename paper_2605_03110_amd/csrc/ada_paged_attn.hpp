@@ -95,6 +95,43 @@ __global__ __launch_bounds__(1024) void k_paged_plan(PagedArgs p, int tile_rows,
     if (tid == 0) { prefix[0] = 0; *tiles = n_tiles; }
 }
 
+// The same for up to 64 sequences and as many tiles as make 16 rounds of one wave: no barriers (six sequences, fp32, 12 x 64: 20.7 -> 19.4 us a call).
+__global__ __launch_bounds__(64) void k_paged_plan_few(PagedArgs p, int tile_rows, int unit, int room, long long* prefix, int2* tile, int* tiles) {
+    const int lane = threadIdx.x;
+    Seq mine = {0, 0, 0, 0};
+    if (lane < p.B) mine = paged_seq(p, lane);
+    long long upto = ((long long)mine.n * p.G + tile_rows - 1) / tile_rows;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const long long u = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += u;
+    }
+    if (upto > room) raise(p, ADA_ERR_SHAPE);
+    const int ends = (int)min(upto, (long long)room), n_tiles = __shfl(ends, 63, 64);     // tiles up to and with sequence `lane`
+    long long front = 0;
+    for (int t0 = 0; t0 < n_tiles; t0 += 64) {
+        const int t = t0 + lane;
+        int b = 0;                                         // the first whose tiles end behind t
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) b += __shfl(ends, b + o - 1, 64) <= t ? o : 0;
+        const int before = __shfl(ends, max(b - 1, 0), 64), j = t - (b > 0 ? before : 0);
+        const int n = __shfl(mine.n, b, 64), past = __shfl(mine.past, b, 64);
+        const int last = (int)min((long long)n - 1, ((long long)(j + 1) * tile_rows - 1) / p.G);
+        long long sum = t < n_tiles ? ((p.causal ? past + last + 1 : past + n) + unit - 1) / unit + BEGIN : 0;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const long long u = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += u;
+        }
+        if (t < n_tiles) {
+            tile[t] = {b, j};
+            prefix[t + 1] = front + sum;
+        }
+        front += __shfl(sum, 63, 64);
+    }
+    if (lane == 0) { prefix[0] = 0; *tiles = n_tiles; }
+}
+
 // A tile of one head, and where it stands in the line.
 struct Tile {
     long long at;
@@ -670,7 +707,11 @@ hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
     if (!chunks && (long long)a.p.longest * a.p.G <= TILE_ROWS) return launch_rows<In, DH, TOKENS>(a, st);
     {
         ProfHook ps(ADA_K_ATTN, st);
-        hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, chunks ? TileGeom<DH>::ROWS : TILE_ROWS, chunks ? TileGeom<DH>::KEYS : UNIT, w.room, prefix, tile, tiles);
+        const int tile_rows = chunks ? TileGeom<DH>::ROWS : TILE_ROWS, unit = chunks ? TileGeom<DH>::KEYS : UNIT;
+        if (a.p.B <= 64 && (long long)a.p.rows * a.p.G / tile_rows + a.p.B <= 1024)
+            hipLaunchKernelGGL(k_paged_plan_few, dim3(1), dim3(64), 0, st, a.p, tile_rows, unit, w.room, prefix, tile, tiles);
+        else
+            hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(1024), 0, st, a.p, tile_rows, unit, w.room, prefix, tile, tiles);
     }
     if (hipError_t e = hipGetLastError()) return e;
     if constexpr (dtype == ADA_BF16)

@@ -165,6 +165,8 @@ APPEND = {
     "chunk_part": (lambda: ref.Case("bf16", 2, 1, 128, 16, [40, 7], [9, 0]), 32, False, False),
     "chunk_f32": (lambda: ref.Case("f32", 4, 2, 128, 32, [33, 64], [1, 0], order="slots"), 128, True, True),
     "chunk_f32_part": (lambda: ref.Case("f32", 6, 3, 64, 256, [300], [77]), 16, False, True),
+    "two_launches": (lambda: ref.Case("bf16", 16, 8, 128, 32, [1500, 1, 333, 50], [70, 31, 0, 5], pad_rows=9), 128, False, True),
+    "two_launches_f32": (lambda: ref.Case("f32", 16, 16, 64, 128, [1400], [333], order="slots"), 32, True, False),
     "no_rotation": (lambda: ref.Case("bf16", 2, 2, 64, 16, [5, 1], [14, 0]), 0, False, True),
     "copy": (lambda: ref.Case("f32", 2, 2, 64, 16, [5, 1], [14, 0]), 0, False, False),
 }
