@@ -269,34 +269,54 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
         if (half == 0) put(a.part_ml + ((slot * G::WAVES + wave) * 32 + l32) * 2, m_run, l);
         int first, last;
         if (!comes_last(a, piece, t, first, last, reinterpret_cast<int*>(lds + 4 * G::STAGE))) continue;
+        // Four parts at a time: every part is a trip to memory, and whoever joins is the last to end (512 tokens behind 16000, heads of 256, four or
+        // five parts a tile: 266 us a call with one part at a time, 229 so).  C blocks of 32 columns at a time, as many as registers hold.
+        constexpr int C = G::PER_CU == 1 ? 2 : 1;
+        auto part_at = [&](int w) { return (2LL * w + (w == first ? 1 : 0)) * G::WAVES + wave; };
         float m = -INFINITY;
-        l = 0.f;
-        for (int w = first; w <= last; ++w) m = fmaxf(m, get(a.part_ml + (((2LL * w + (w == first ? 1 : 0)) * G::WAVES + wave) * 32 + l32) * 2)[0]);
+        for (int w0 = first; w0 <= last; w0 += 4) {
+            float mw[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mw[q] = get(a.part_ml + (part_at(min(w0 + q, last)) * 32 + l32) * 2)[0];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) m = fmaxf(m, mw[q]);
+        }
         uint16_t* to = reinterpret_cast<uint16_t*>(a.out) + row * a.ld_out + (long long)(t.kvh * p.G + head) * DH + 4 * half;
 #pragma unroll 1
-        for (int i = 0; i < NB; ++i) {                     // 32 columns at a time: the other registers stay the loop's
-            float o[16];
+        for (int i = 0; i < NB; i += C) {
+            float o[C][16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = 0.f;
+            for (int e = 0; e < 16 * C; ++e) o[e >> 4][e & 15] = 0.f;
             l = 0.f;
-            for (int w = first; w <= last; ++w) {
-                const long long s2 = (2LL * w + (w == first ? 1 : 0)) * G::WAVES + wave;
-                const f32x2 ml = get(a.part_ml + (s2 * 32 + l32) * 2);
-                const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
-                l += ml[1] * f;
-                const float* from = a.part_o + s2 * (32 * DH) + 2 * lane + i * 16 * 64;
+            for (int w0 = first; w0 <= last; w0 += 4) {
+                f32x2 ml[4], v[4][C][8];
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const f32x2 v = get(from + e * 64);
-                    o[e] += v[0] * f;
-                    o[e + 1] += v[1] * f;
+                for (int q = 0; q < 4; ++q) {
+                    const long long s2 = part_at(min(w0 + q, last));
+                    ml[q] = get(a.part_ml + (s2 * 32 + l32) * 2);
+                    const float* from = a.part_o + s2 * (32 * DH) + 2 * lane + i * 16 * 64;
+#pragma unroll
+                    for (int e = 0; e < 8 * C; ++e) v[q][e >> 3][e & 7] = get(from + e * 128);
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float f = w0 + q > last || ml[q][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[q][0] - m);
+                    l += ml[q][1] * f;
+#pragma unroll
+                    for (int e = 0; e < 8 * C; ++e) {
+                        o[e >> 3][2 * (e & 7)] += v[q][e >> 3][e & 7][0] * f;
+                        o[e >> 3][2 * (e & 7) + 1] += v[q][e >> 3][e & 7][1] * f;
+                    }
                 }
             }
             const float f = l > 0.f ? 1.f / l : 0.f;
             if (mine)
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    *reinterpret_cast<u32x2*>(to + 32 * i + 8 * w) = u32x2{bf16_pair(o[4 * w] * f, o[4 * w + 1] * f), bf16_pair(o[4 * w + 2] * f, o[4 * w + 3] * f)};
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        *reinterpret_cast<u32x2*>(to + 32 * (i + c) + 8 * w) =
+                            u32x2{bf16_pair(o[c][4 * w] * f, o[c][4 * w + 1] * f), bf16_pair(o[c][4 * w + 2] * f, o[c][4 * w + 3] * f)};
         }
     }
 }
