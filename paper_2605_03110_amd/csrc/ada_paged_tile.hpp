@@ -300,7 +300,8 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
                 }
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float f = w0 + q > last || ml[q][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[q][0] - m);
+                    if (w0 + q > last) break;
+                    const float f = ml[q][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[q][0] - m);
                     l += ml[q][1] * f;
 #pragma unroll
                     for (int e = 0; e < 8 * C; ++e) {
