@@ -237,12 +237,22 @@ template <int MODE> struct Line {
     }
 };
 
-// The workgroup's piece of the line: x0 .. x1 - 1 of `pieces`.
+// The shortest piece worth having, for tiles of so many units: the workgroups of a tile do units / parts of its work beside each other, the one that joins takes
+// the parts one after the other, and a part costs it about what a unit does (16-row tiles: a quarter): least where parts = sqrt(units).  us a call with
+// a piece for every workgroup and so: one token at 8000 keys, 32 x 128 over 8, 23.6 and 16.5; with 16 x 256 over 8 58.6 and 31.8; 64 rows of two heads at 8000 keys in
+// 128-row tiles 92 and 41.
+__device__ inline long long least_of(float units) { return max((long long)__builtin_sqrtf(units), 1LL); }
+
+// The workgroup's piece of the line: x0 .. x1 - 1 of `pieces`.  Where not every workgroup could have `many` of the shortest, one per CU gets a piece: two of
+// them on a CU run at half the rate each, and the parts would be twice as many.  16-row tiles, 4 (fp32 2): 16 sequences with 32 listed pages 32.1 -> 28.5 us a call, 4 tokens at
+// 8000 keys 32.2 -> 28.5.  128-row tiles: 1, and 2 with heads of 128: 512 rows at 8000 keys 71 -> 50, eight times 128 rows 82 -> 71.
 struct Piece {
     long long total, x0, x1;
     int me, pieces;
-    __device__ explicit Piece(long long length) : total(length) {
-        pieces = (int)min((long long)gridDim.x, total);    // (none is empty)
+    __device__ Piece(long long length, long long least, int per_cu, int many) : total(length) {
+        long long most = total / least;
+        if (most < (long long)many * gridDim.x) most = min(most, (long long)gridDim.x / per_cu);
+        pieces = (int)max(min((long long)gridDim.x, most), 1LL);               // (none is empty)
         me = pieces == (int)gridDim.x ? by_xcd(blockIdx.x, pieces) : (int)blockIdx.x;
         x0 = me < pieces ? from(me) : 0;
         x1 = me < pieces ? from(me + 1) : 0;
@@ -354,7 +364,7 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
     int* flag = reinterpret_cast<int*>(lbuf + 4 * TILE_ROWS);
     const Line<MODE> line(a);
     if (line.total == 0) return;
-    const Piece piece(line.total);
+    const Piece piece(line.total, least_of(0.25f * (float)line.per_head / (MODE == CHUNKS ? *a.tiles : MODE == TOKENS ? p.B : p.rows)), 2, sizeof(In) == 2 ? 4 : 2);
 
     for (long long x = piece.x0; x < piece.x1;) {
         const Tile t = line.find(x);
@@ -642,8 +652,16 @@ __global__ __launch_bounds__(256, DH * sizeof(In) > 256 ? 1 : 2) void k_paged_ro
 // ------------------------------------------------------------------------------------------------ host
 struct AttendWs { size_t tiles, prefix, tile, part_o, part_ml, bytes; int room; };
 
-// Chunks whose rows fill a good part of a 128-row tile go to ada_paged_tile.hpp's kernel.
-inline bool takes_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G >= 48; }
+// Chunks in bf16 go to ada_paged_tile.hpp's kernel where they have more than 16 rows a sequence and 16-row tiles enough for half of the CUs (heads of 256,
+// whose 16-row tiles take twice the registers: a sixth): with fewer, no tile of 128 rows has work for a CU that its parts' join does not cost
+// again.  us a call with 16-row and 128-row tiles, 32 x 128 over 8 at 8000 keys: 128 16-row tiles in one sequence 40 and 48, in eight 61 and 82; 256 in one 56 and 50,
+// in eight 96 and 75; 1536 in 24 413 and 173; at 1000 keys 128 in one 18 and 26, 768 in 24 52 and 36.  16 x 256 over 8: 32 27.6 and 46, 96 133 and 77.
+inline bool may_take_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G > TILE_ROWS; }   // (what grows with the chunk)
+inline bool takes_tiles(const PagedArgs& p, int d_h, int dtype) {
+    const long long rows = (long long)p.rows * p.G;
+    return may_take_tiles(p, dtype) && rows > (long long)TILE_ROWS * p.B &&
+           rows / TILE_ROWS * p.H_kv > ada_hook_cus() / (d_h > 128 ? 6 : 2);
+}
 
 // Two workgroups per CU: 64 single tokens at 100 to 8191 keys, 32 x 128 over 8, us a call with 1, 2, 3, 4 of them: 101, 102, 118, 111 (registers hold two at
 // once); 1024 tokens with 16 listed pages of 64: 597, 422, 477, 422.
@@ -652,7 +670,7 @@ inline int tile_pieces(int d_h) { const int n = (d_h > 128 ? 1 : 2) * ada_hook_c
 
 inline AttendWs attend_ws(const PagedArgs& p, int d_h, int dtype) {
     const size_t tiles = (size_t)((long long)p.rows * p.G / TILE_ROWS + p.B);
-    const size_t rows = (size_t)rows_pieces() * TILE_ROWS, tile_rows = takes_tiles(p, dtype) ? (size_t)tile_pieces(d_h) * 128 : 0;
+    const size_t rows = (size_t)rows_pieces() * TILE_ROWS, tile_rows = may_take_tiles(p, dtype) ? (size_t)tile_pieces(d_h) * 128 : 0;
     const size_t parts = 2 * (rows > tile_rows ? rows : tile_rows);           // rows of cut tiles (listed pages always take 16-row ones)
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     AttendWs w;
@@ -703,7 +721,7 @@ hipError_t launch_attend(AttendArgs a, void* ws, hipStream_t st) {
     a.part_o = reinterpret_cast<float*>(at + w.part_o);
     a.part_ml = reinterpret_cast<float*>(at + w.part_ml);
     if (a.list) return launch_rows<In, DH, LISTED>(a, st);
-    const bool chunks = takes_tiles(a.p, dtype);
+    const bool chunks = takes_tiles(a.p, DH, dtype);
     if (!chunks && (long long)a.p.longest * a.p.G <= TILE_ROWS) return launch_rows<In, DH, TOKENS>(a, st);
     {
         ProfHook ps(ADA_K_ATTN, st);

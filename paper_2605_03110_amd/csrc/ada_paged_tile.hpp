@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
     const bool young = blockIdx.x >= gridDim.x / 2;
     const Line<CHUNKS> line(a);
     if (line.total == 0) return;
-    const Piece piece(line.total);
+    const Piece piece(line.total, least_of((float)line.per_head / *a.tiles), G::PER_CU, DH == 128 ? 2 : 1);
     // where this lane's columns of a value row start in LDS for the transposed reads: rows 4 half + (lane & 15) / 4 + 8 n, columns 16 ((lane >> 4) & 1) + 4 (lane & 3)
     const int vrow = 4 * half + ((lane & 15) >> 2);
     const int vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(256, TileGeom<DH>::PER_CU) void k_paged_tile(Attend
         if (!comes_last(a, piece, t, first, last, reinterpret_cast<int*>(lds + 4 * G::STAGE))) continue;
         // Four parts at a time: every part is a trip to memory, and whoever joins is the last to end (512 tokens behind 16000, heads of 256, four or
         // five parts a tile: 266 us a call with one part at a time, 229 so).  C blocks of 32 columns at a time, as many as registers hold.
-        constexpr int C = G::PER_CU == 1 ? 2 : 1;
+        constexpr int C = DH == 128 ? 1 : 2;
         auto part_at = [&](int w) { return (2LL * w + (w == first ? 1 : 0)) * G::WAVES + wave; };
         float m = -INFINITY;
         for (int w0 = first; w0 <= last; w0 += 4) {

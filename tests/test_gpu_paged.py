@@ -74,6 +74,55 @@ def test_attention(pa, name, causal):
     check_attend(c, out, causal)
 
 
+# enough rows for the tiles of 128 rows on any number of CUs up to 256 (more than half as many tiles of 16 rows as CUs)
+TILES = {
+    "group_4": lambda: ref.Case("bf16", 32, 8, 128, 16, [77], [100], pad_rows=3),
+    "heads_64": lambda: ref.Case("bf16", 12, 2, 64, 32, [200, 129], [0, 511], order="slots"),
+    "heads_256": lambda: ref.Case("bf16", 8, 4, 256, 64, [150], [333]),
+    "heads_256_many_parts": lambda: ref.Case("bf16", 8, 2, 256, 16, [101], [3000], order="slots"),
+    "mixed": lambda: ref.Case("bf16", 16, 4, 128, 16, [1, 0, 33, 300, 1, 0, 2], [40, 9, 0, 17, 513, 0, 64], pad_rows=5),
+    "large_scores": lambda: ref.Case("bf16", 16, 8, 128, 32, [160, 1], [70, 400], scale=8.0),
+    "many_parts": lambda: ref.Case("bf16", 64, 4, 64, 16, [40], [9000]),
+    "many_sequences": lambda: ref.Case("bf16", 16, 2, 64, 32, [(b * 7) % 23 for b in range(130)], [(37 * b) % 200 for b in range(130)]),
+    "values_off_zero": lambda: ref.Case("bf16", 16, 4, 128, 16, [164, 1], [0, 900], value_shift=3.0),
+}
+
+
+@pytest.mark.parametrize("causal", (True, False))
+@pytest.mark.parametrize("name", TILES)
+def test_attention_in_tiles(pa, name, causal):
+    """Twice over one workspace, which is found as it was left: a batch with chunks of more rows."""
+    c = TILES[name]()
+    cache, chunk = c.on_gpu(pa)
+    ws = pa.paged_workspace(cache, chunk, c.H)
+    ws[pa.PAGED_ZERO_BYTES:].fill_(255)
+    first = None
+    for _ in range(2):
+        out = torch.full((c.rows, c.H * c.d_h), 7.0, dtype=c.dtype, device="cuda")
+        res = pa.ada_attention_paged(cache, chunk, c.Q.cuda(), out=out, ws=ws, flags=pa.FLAG_ATTN_CAUSAL if causal else 0)
+        assert res["status"].item() == OK
+        assert bool((out[int(c.start[-1]):] == 7.0).all()), "rows behind the last sequence"
+        assert bool((ws[:pa.PAGED_ZERO_BYTES] == 0).all())
+        assert first is None or torch.equal(first, out)
+        first = out
+    check_attend(c, first, causal)
+
+
+def test_tiles_of_strided_rows_with_pages_outside_the_pool(pa):
+    c = ref.Case("bf16", 32, 8, 128, 16, [1, 1, 90], [100, 15, 0])
+    c.table[0, 2] = c.pages
+    c.table[1, 0] = -1                                     # all that this row sees
+    c.table[2, 1] = 2 ** 31 - 1
+    cache, chunk = c.on_gpu(pa)
+    wide = torch.full((c.rows, 34 * 128), math.nan, dtype=c.dtype, device="cuda")
+    wide[:, 128:33 * 128] = c.Q.cuda()
+    out = torch.full((c.rows, 33 * 128), 7.0, dtype=c.dtype, device="cuda")
+    res = pa.ada_attention_paged(cache, chunk, wide[:, 128:33 * 128], out=out[:, 128:], flags=pa.FLAG_ATTN_CAUSAL)
+    assert res["status"].item() == INDEX
+    assert bool((out[:, :128] == 7.0).all()) and bool((out[1, 128:] == 0).all())
+    check_attend(c, out[:, 128:], True, drop=((0, 2), (1, 0), (2, 1)))
+
+
 def test_attention_of_strided_rows(pa):
     c = ref.Case("bf16", 4, 2, 64, 16, [20, 1], [33, 80])
     cache, chunk = c.on_gpu(pa)
