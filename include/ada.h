@@ -517,7 +517,8 @@ int ada_cascade_report(int L, int T, const int32_t* counts_all, const uint64_t* 
  * two HIP events recorded on the stream it is launched on.  ada_profile_collect waits for them and returns,
  * per kernel class, the summed elapsed milliseconds and the number of launches since the last collect
  * (HOST arrays of ADA_K_COUNT entries), then forgets them.  Event pairs include the launch gap in front of the
- * kernel, so these figures are upper bounds of the durations a kernel trace reports.
+ * kernel, so these figures are upper bounds of the durations a kernel trace reports.  The calls over a paged cache count as
+ * ADA_K_ATTN, whatever they launch.
  */
 enum { ADA_K_NORM_PREP = 0, ADA_K_GRAM_FULL = 1, ADA_K_GRAM_REP = 2, ADA_K_GRAM_CROSS = 3, ADA_K_UPDATE = 4,
        ADA_K_CASCADE_FUSED = 5, ADA_K_MFMA_PROBE = 6, ADA_K_ASSIGN = 7, ADA_K_ATTN = 8, ADA_K_SCREEN = 9, ADA_K_COUNT = 10 };

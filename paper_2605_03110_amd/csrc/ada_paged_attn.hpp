@@ -654,8 +654,8 @@ struct AttendWs { size_t tiles, prefix, tile, part_o, part_ml, bytes; int room; 
 
 // Chunks in bf16 go to ada_paged_tile.hpp's kernel where they have more than 16 rows a sequence and 16-row tiles enough for half of the CUs (heads of 256,
 // whose 16-row tiles take twice the registers: a sixth): with fewer, no tile of 128 rows has work for a CU that its parts' join does not cost
-// again.  us a call with 16-row and 128-row tiles, 32 x 128 over 8 at 8000 keys: 128 16-row tiles in one sequence 40 and 48, in eight 61 and 82; 256 in one 56 and 50,
-// in eight 96 and 75; 1536 in 24 413 and 173; at 1000 keys 128 in one 18 and 26, 768 in 24 52 and 36.  16 x 256 over 8: 32 27.6 and 46, 96 133 and 77.
+// again.  us a call with 16-row and 128-row tiles, 32 x 128 over 8 at 8000 keys: 64 16-row tiles in one sequence 36 and 48, 128 57 and 50; 256 in eight
+// 96 and 71; 1536 in 24 413 and 173; at 1000 keys 128 in one 18 and 27, 768 in 24 52 and 36.  16 x 256 over 8 at 8000 keys: 32 in one 56 and 77, 64 104 and 80.
 inline bool may_take_tiles(const PagedArgs& p, int dtype) { return dtype == ADA_BF16 && (long long)p.longest * p.G > TILE_ROWS; }   // (what grows with the chunk)
 inline bool takes_tiles(const PagedArgs& p, int d_h, int dtype) {
     const long long rows = (long long)p.rows * p.G;
