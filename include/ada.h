@@ -448,7 +448,8 @@ int ada_cache_append(const ada_paged_cache* cache, const ada_paged_chunk* chunk,
  * Chunks and single tokens, in any mixture.
  *   Q     rows x (H d_h), the cache's dtype, leading dimension ldq, 16-byte aligned rows
  *   out   rows x (H d_h), the cache's dtype, leading dimension ld_out, 16-byte aligned rows.  A row that sees no key is 0
- * Sums, maxima and (fp32 caches) all products in fp32.  What lies behind a sequence's last token is never read.
+ * Sums, maxima and (fp32 caches) all products in fp32.  What lies behind a sequence's last token is never read.  Numbers are taken to be
+ * finite: an infinity or NaN among a sequence's keys and values may reach all rows of that sequence, those that do not see it too, and no others.
  */
 int ada_attention_paged(const ada_paged_cache* cache, const ada_paged_chunk* chunk, const void* Q, int H, int64_t ldq,
                         void* out, int64_t ld_out, int32_t* status, void* ws, size_t ws_bytes, void* stream, unsigned flags);

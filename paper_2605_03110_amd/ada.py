@@ -6,6 +6,7 @@ result to the host and raises on a device-reported status.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import subprocess
@@ -787,9 +788,15 @@ def _paged_rows(cache: PagedCache, chunk: Chunk, X: torch.Tensor, name: str, hea
     return n, ld if rows > 1 else width                    # (one row steps nowhere)
 
 
-def _paged_status(cache: PagedCache, status: Optional[torch.Tensor]) -> torch.Tensor:
+def _made_on(stream):
+    """What a call makes for itself is filled, and its memory goes back, on the stream that the call works on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _paged_status(cache: PagedCache, status: Optional[torch.Tensor], stream) -> torch.Tensor:
     if status is None:
-        return torch.zeros(1, dtype=torch.int32, device=cache.device)
+        with _made_on(stream):
+            return torch.zeros(1, dtype=torch.int32, device=cache.device)
     if status.dtype is not torch.int32 or status.device != cache.device or status.numel() < 1:
         raise ValueError("status must be an int32 tensor on the cache's device")
     return status
@@ -826,11 +833,12 @@ def ada_cache_append(cache: PagedCache, chunk: Chunk, Q: Optional[torch.Tensor],
             raise ValueError("rope must be a contiguous float32 [positions, rot / 2, 2] device tensor")
         positions, half, _ = rope.shape
         rot = 2 * half
-    status = _paged_status(cache, status)
+    status = _paged_status(cache, status, stream)
     if Q is None:
         out = None
     elif out is None:
-        out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        with _made_on(stream):
+            out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
         ldo = Q.shape[1]
     else:
         ldo = _paged_rows(cache, chunk, out, "out", H)[1]
@@ -842,10 +850,13 @@ def ada_cache_append(cache: PagedCache, chunk: Chunk, Q: Optional[torch.Tensor],
 
 def _paged_attention(cache, chunk, Q, lists, ws, out, status, stream, flags, name):
     H, ldq = _paged_rows(cache, chunk, Q, "Q")
-    status = _paged_status(cache, status)
-    ws = paged_workspace(cache, chunk, H) if ws is None else ws
+    status = _paged_status(cache, status, stream)
+    if ws is None:
+        with _made_on(stream):
+            ws = paged_workspace(cache, chunk, H)
     if out is None:
-        out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        with _made_on(stream):
+            out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
         ldo = Q.shape[1]
     else:
         ldo = _paged_rows(cache, chunk, out, "out", H)[1]
@@ -886,15 +897,18 @@ def ada_select_pages(cache: PagedCache, chunk: Chunk, Q: torch.Tensor, budget: i
     H, ldq = _paged_rows(cache, chunk, Q, "Q")
     if cache.bounds is None:
         raise ValueError("the cache has no bounds to score pages by")
-    status = _paged_status(cache, status)
+    status = _paged_status(cache, status, stream)
     if out is None:
-        out = dict(pages=torch.empty((chunk.rows, cache.H_kv, int(budget)), dtype=torch.int32, device=cache.device),
-                   counts=torch.empty((chunk.rows, cache.H_kv), dtype=torch.int32, device=cache.device))
+        with _made_on(stream):
+            out = dict(pages=torch.empty((chunk.rows, cache.H_kv, int(budget)), dtype=torch.int32, device=cache.device),
+                       counts=torch.empty((chunk.rows, cache.H_kv), dtype=torch.int32, device=cache.device))
     pages, counts = out["pages"], out["counts"]
     _check_lists(cache, chunk, pages, counts)
     if pages.shape[2] != budget:
         raise ValueError("pages must have `budget` entries per row and head")
-    ws = paged_workspace(cache, chunk, H) if ws is None else ws
+    if ws is None:
+        with _made_on(stream):
+            ws = paged_workspace(cache, chunk, H)
     _paged_call(cache, chunk, lambda: lib().ada_select_pages(
         cache.ref, chunk.ref, Q.data_ptr(), H, ldq, budget, first, last, pages.data_ptr(), counts.data_ptr(), status.data_ptr(), ws.data_ptr(), ws.numel(),
         _stream(stream), flags), "ada_select_pages")

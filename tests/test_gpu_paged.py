@@ -157,6 +157,24 @@ def test_pages_outside_the_pool_count_as_masked(pa):
     check_attend(c, res["out"], True, drop=((0, 2), (1, 0), (2, 1)))
 
 
+@pytest.mark.parametrize("make", (lambda: ref.Case("bf16", 8, 2, 128, 16, [1] * 6, [100, 300, 15, 7, 1000, 40]),
+                                  lambda: ref.Case("f32", 4, 2, 64, 16, [1] * 6, [100, 300, 15, 7, 1000, 40]),
+                                  lambda: ref.Case("bf16", 32, 8, 128, 16, [30, 20, 1, 50, 2, 3], [100, 300, 15, 7, 1000, 40])))
+def test_numbers_that_are_none_stay_in_their_sequence(pa, make):
+    c = make()
+    cache, chunk = c.on_gpu(pa)
+    for b, value in ((1, math.nan), (4, math.inf)):
+        for pages in (cache.K, cache.V):
+            pages[c.table[b, 0].item()][:, 3] = value
+            pages[c.table[b, 0].item()][:, 5] = -value
+    out = pa.ada_attention_paged(cache, chunk, c.Q.cuda(), flags=pa.FLAG_ATTN_CAUSAL)["out"].double().cpu()
+    want, weight, err = ref.attend(c, True)
+    room = ref.tolerance(c, want, weight, err, step_of(c))
+    for b in (0, 2, 3, 5):
+        rows = slice(int(c.start[b]), int(c.start[b + 1]))
+        assert bool(((out - want).abs() <= room)[rows].all()), b
+
+
 def test_sequences_that_do_not_fit_are_left_out(pa):
     c = ref.Case("bf16", 4, 2, 64, 16, [3, 1, 2], [20, 7, 30])
     for what in ("past", "long", "behind"):
@@ -566,6 +584,30 @@ def test_two_calls_at_once(pa):
         torch.cuda.synchronize()
     for c, r in zip(cases, got):
         check_attend(c, r["out"], True)
+
+
+def test_calls_on_a_given_stream_make_what_they_need_on_it(pa):
+    """The current stream is busy and its memory was used before: status, workspace and outputs of calls on another stream do not wait for it."""
+    c = ref.Case("bf16", 8, 2, 128, 32, [1] * 4, [900, 10, 300, 1024], seed=3)
+    cache, chunk = c.on_gpu(pa)
+    q, side, busy = c.Q.cuda(), torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    want = pa.ada_select_pages(cache, chunk, q, 4)
+    want = [want["pages"].clone(), want["counts"].clone(), pa.ada_attention_pages(cache, chunk, q, want["pages"], want["counts"])["out"].clone()]
+    n = pa.ada_paged_workspace_bytes(cache, chunk, c.H)
+    used = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    del used
+    for _ in range(20):
+        busy = busy @ busy * 1e-3
+    sel = pa.ada_select_pages(cache, chunk, q, 4, stream=side)
+    res = pa.ada_attention_pages(cache, chunk, q, sel["pages"], sel["counts"], stream=side)
+    full = pa.ada_attention_paged(cache, chunk, q, stream=side)
+    side.synchronize()
+    assert [r["status"].item() for r in (sel, res, full)] == [OK] * 3
+    for a, b in zip(want, (sel["pages"], sel["counts"], res["out"])):
+        assert torch.equal(a, b)
+    check_attend(c, full["out"], False)
+    torch.cuda.synchronize()
 
 
 def test_offsets_past_32_bits(pa):
