@@ -253,7 +253,7 @@ struct Piece {
         long long most = total / least;
         if (most < (long long)many * gridDim.x) most = min(most, (long long)gridDim.x / per_cu);
         pieces = (int)max(min((long long)gridDim.x, most), 1LL);               // (none is empty)
-        me = pieces == (int)gridDim.x ? by_xcd(blockIdx.x, pieces) : (int)blockIdx.x;
+        me = (int)blockIdx.x < pieces ? by_xcd(blockIdx.x, pieces) : (int)blockIdx.x;
         x0 = me < pieces ? from(me) : 0;
         x1 = me < pieces ? from(me + 1) : 0;
     }
